@@ -55,8 +55,9 @@ typedef enum {
     SIK_ERR_WORKSPACE = -6, /* workspace NULL, misaligned or smaller than sik_workspace_bytes */
     SIK_ERR_LAUNCH = -7,    /* the HIP runtime reported an error while enqueueing           */
     SIK_ERR_FLAGS = -8,     /* unknown quantiser mode, or an option value out of range      */
-    SIK_ERR_STATIC_LIMIT = -9 /* sik_decode_step_static: the layout needs more scratch memory than the
+    SIK_ERR_STATIC_LIMIT = -9, /* sik_decode_step_static: the layout needs more scratch memory than the
                                  library's built-in buffer holds (SIK_STATIC_SCRATCH_BYTES)       */
+    SIK_ERR_ALIGN = -10     /* a pointer or stride of the prompt-side calls is not 16-byte aligned        */
 } sik_status;
 
 /* Shape of one attention layer's cache.  head_dim must be 128 (the head size of every
@@ -331,6 +332,118 @@ typedef struct {
 } sik_decode_args;
 
 int sik_decode_step_ex(const sik_layout *layout, const sik_decode_args *args);
+
+/* ---- the prompt side of the cache -------------------------------------------------------------------------------
+ * What puts keys and values into the cache that the calls above compress and decode from, and what chooses the tokens
+ * that stay: per-head norms with the position rotation (sik_rope_append), attention of a chunk of new tokens over the
+ * cache (sik_chunk_attn), the attention weight that each cached token receives (sik_attn_mass) and eviction by it
+ * (sik_evict), whose list also serves as the forced set of sik_decode_step_ex (section "Full Precision Sink Tokens").
+ *
+ * The cache of these calls is contiguous, K, V [B, Hkv, max_len, D] as above, or paged: pools [n_pages, Hkv, page_len, D]
+ * and a table that names the pages of each sequence in order: token j of sequence b is row j % page_len of page
+ * page_table[b][j / page_len].  A page may appear in the tables of several sequences (a shared prefix).  Entries outside
+ * [0, n_pages) name no page: rows of such tokens are neither read nor written, and the tokens take no part in attention.
+ * max_len bounds the length of a sequence in either case.
+ *
+ * A chunk is n new tokens per sequence, of which sequence b has n_new[b] (values are clamped to [0, n]); rows of the
+ * chunk's tensors at or beyond n_new[b] are neither read nor written.  seq_len[b] (clamped to [0, max_len]) is the number
+ * of tokens in the cache BEFORE the chunk; token t of the chunk is cache row seq_len[b] + t, and tokens at or beyond
+ * max_len are dropped (not written, and as queries their output rows are left as they were).  No call
+ * here changes seq_len: add n_new to it once the chunk went through the layers.
+ *
+ * Both blocks are host structures that hold device pointers; zero-initialise them and set what applies. */
+typedef struct {
+    const int32_t *page_table; /* [B, pages_per_seq] (device) */
+    int32_t pages_per_seq;     /* pages_per_seq * page_len >= max_len */
+    int32_t page_len;          /* a power of two, at least 16 */
+    int32_t n_pages;
+} sik_pages;
+
+typedef struct {
+    int32_t n;              /* token rows per sequence in the chunk's tensors, 1 <= n <= max_len */
+    const int32_t *n_new;   /* [B] (device), NULL: n for every sequence */
+    const int32_t *seq_len; /* [B] (device) */
+    const sik_pages *pages; /* (host) NULL: contiguous */
+} sik_chunk;
+
+/* Norms of the queries and keys of a chunk for each head, position rotation, and the keys and values into the cache, in
+ * one pass.  For every head row x (D values) of q [B,n,Hq,D] and k [B,n,Hkv,D]:
+ *   y = x * w / sqrt(mean(x^2) + eps)     w = q_weight / k_weight [D] float; NULL: y = x
+ *   channels (a, b) of pair i: a cos(f) - b sin(f), a sin(f) + b cos(f)   with f = position * inv_freq[i]
+ * inv_freq [rotary_dim / 2] float; rotary_dim is a multiple of 16 from 16 to D (or 0: nothing is rotated, inv_freq NULL);
+ * pair i is channels (i, i + rotary_dim / 2), or (2i, 2i + 1) with interleaved = 1; channels from rotary_dim on are not
+ * rotated.  position = seq_len[b] + t, or positions[b][t] ([B,n] int32) where given (a cache that tokens were evicted
+ * from: rows and positions differ).  The angle is the exact product, reduced to a turn in 64 bits; everything else is
+ * binary32, rounded once to kv_dtype.
+ * Tokens of q, k and v lie q_stride, k_stride, v_stride elements apart (0: packed, heads * D), sequences n times that, so
+ * that they may be parts of one projection's output; a head's D values and the heads of a token are contiguous.
+ * q_out [B,n,Hq,D].  Keys go to k_out [B,n,Hkv,D] (a decode step's k_new, v then is used as it is: v = K = V = NULL) or,
+ * with the values of v, into the cache K, V (k_out = NULL).  Outputs must not overlap inputs (q_out = q and k_out = k are
+ * refused: a row is read by other lanes than the ones that write it). */
+typedef struct {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    const float *q_weight, *k_weight;
+    float eps;
+    const float *inv_freq;
+    int32_t rotary_dim;
+    int32_t interleaved;
+    const int32_t *positions;
+    void *q_out, *k_out;
+    void *K, *V;
+    void *stream;
+} sik_rope_args;
+
+int sik_rope_append(const sik_layout *layout, const sik_chunk *chunk, const sik_rope_args *args);
+
+/* Bytes of scratch memory that sik_chunk_attn and sik_evict need for this layout and chunks of up to n tokens (0 if the
+ * layout or n is invalid).  Contents are not preserved and need no initialisation; the same buffer may serve every call on
+ * one stream, calls sharing it must not overlap in time. */
+size_t sik_chunk_workspace_bytes(const sik_layout *layout, int32_t n);
+
+/* Attention of the chunk's queries over the cache, in which the chunk's own rows already lie (sik_rope_append):
+ *   out[b,t,hq] = sum_j p_j V_j, p = softmax over the tokens j <= seq_len[b] + t of softmax_scale * q[b,t,hq] . K_j
+ * q [B,n,Hq,D] kv_dtype, out [B,n,Hq,D] out_dtype, lse [B,n,Hq] float or NULL: the natural logarithm of the softmax's
+ * sum.  softmax_scale <= 0 means 1 / sqrt(D).  A row without any token (all its pages are unmapped) gives a zero row and
+ * lse = -infinity.  Products on the matrix units with binary32 sums.  K, V and q must be finite in every valid row. */
+int sik_chunk_attn(const sik_layout *layout, const sik_chunk *chunk, const void *q, const void *K, const void *V,
+                   float softmax_scale, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Attention weight that each cached token receives from the last n_obs queries of the chunk, summed over the query heads
+ * of its KV head: for j < seq_len[b] + n_new[b]
+ *   mass[b,h,j] = before[b,h,j] + sum over t >= n_new[b] - n_obs, t >= 0, j <= seq_len[b] + t, and hq / R = h of
+ *                 exp(softmax_scale * q[b,t,hq] . K_j - lse[b,t,hq])
+ * mass, before [B,Hkv,max_len] float; before = NULL: 0; before = mass adds in place.  Entries beyond the sequence are left
+ * as they were; tokens on unmapped pages receive nothing.  lse as written by sik_chunk_attn (a row with -infinity
+ * contributes nothing); 1 <= n_obs <= n. */
+int sik_attn_mass(const sik_layout *layout, const sik_chunk *chunk, const void *q, const void *K, float softmax_scale,
+                  const float *lse, int32_t n_obs, const float *before, float *mass, void *stream);
+
+/* Eviction: per (sequence, KV head) the n_keep tokens that stay, L = seq_len[b] (clamped to [0, max_len]): the first n_sink, the last n_recent and of
+ * those between them the n_keep - n_sink - n_recent with the largest mass [B,Hkv,max_len] (equal masses: the smaller
+ * index first; no NaN).  With L <= n_keep every token stays.  keep [B,Hkv,n_keep] int32 receives them in ascending order,
+ * -1 beyond; new_len [B] (may be NULL) min(L, n_keep).  n_sink, n_recent >= 0, n_sink + n_recent <= n_keep <= max_len.
+ * With K_out and V_out (both or neither) the cache is cut down as well: rows keep[b,h,i] of K, V (contiguous, or paged by
+ * `pages`; a token on an unmapped page gives a zero row) become rows i of K_out, V_out [B,Hkv,out_len,D], out_len >=
+ * n_keep; rows beyond new_len are left as they were.  mass_out [B,Hkv,out_len] (may be NULL) receives their masses.  The
+ * outputs must not overlap the inputs.  workspace: sik_chunk_workspace_bytes of the layout and any n. */
+typedef struct {
+    const float *mass;
+    const int32_t *seq_len;
+    int32_t n_keep, n_sink, n_recent;
+    int32_t *keep;
+    int32_t *new_len;
+    const void *K, *V;
+    const sik_pages *pages;
+    void *K_out, *V_out;
+    float *mass_out;
+    int32_t out_len;
+    void *workspace;
+    size_t workspace_bytes;
+    void *stream;
+} sik_evict_args;
+
+int sik_evict(const sik_layout *layout, const sik_evict_args *args);
 
 #ifdef __cplusplus
 }

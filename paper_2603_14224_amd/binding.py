@@ -20,7 +20,8 @@ _TORCH2SIK = {torch.float16: SIK_F16, torch.bfloat16: SIK_BF16, torch.float32: S
 EXPORTS = ("sik_strerror", "sik_version", "sik_plan_info", "sik_workspace_bytes", "sik_workspace_init",
            "sik_workspace_status", "sik_quantize_keys", "sik_score",
            "sik_topk", "sik_sparse_attn", "sik_decode_step", "sik_decode_step_static", "sik_decode_step_profiled", "sik_kvq_bytes",
-           "sik_quantize_kv", "sik_prefill_compress", "sik_sparse_attn_q2", "sik_decode_step_q2", "sik_decode_step_ex")
+           "sik_quantize_kv", "sik_prefill_compress", "sik_sparse_attn_q2", "sik_decode_step_q2", "sik_decode_step_ex",
+           "sik_rope_append", "sik_chunk_workspace_bytes", "sik_chunk_attn", "sik_attn_mass", "sik_evict")
 
 
 class SikError(RuntimeError):
@@ -47,6 +48,38 @@ class Layout(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("max_len", ctypes.c_int32), ("kv_dtype", ctypes.c_int32),
                 ("out_dtype", ctypes.c_int32)]
+
+
+class Pages(ctypes.Structure):
+    """sik_pages of include/sik.h (make_pages keeps the tensor it points to alive)."""
+    _fields_ = [("page_table", ctypes.c_void_p), ("pages_per_seq", ctypes.c_int32), ("page_len", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32)]
+
+
+class Chunk(ctypes.Structure):
+    """sik_chunk of include/sik.h (make_chunk keeps what it points to alive)."""
+    _fields_ = [("n", ctypes.c_int32), ("n_new", ctypes.c_void_p), ("seq_len", ctypes.c_void_p),
+                ("pages", ctypes.POINTER(Pages))]
+
+
+class RopeArgs(ctypes.Structure):
+    """sik_rope_args of include/sik.h."""
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("q_weight", ctypes.c_void_p),
+                ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float), ("inv_freq", ctypes.c_void_p),
+                ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("positions", ctypes.c_void_p),
+                ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p), ("K", ctypes.c_void_p), ("V", ctypes.c_void_p),
+                ("stream", ctypes.c_void_p)]
+
+
+class EvictArgs(ctypes.Structure):
+    """sik_evict_args of include/sik.h."""
+    _fields_ = [("mass", ctypes.c_void_p), ("seq_len", ctypes.c_void_p), ("n_keep", ctypes.c_int32),
+                ("n_sink", ctypes.c_int32), ("n_recent", ctypes.c_int32), ("keep", ctypes.c_void_p),
+                ("new_len", ctypes.c_void_p), ("K", ctypes.c_void_p), ("V", ctypes.c_void_p),
+                ("pages", ctypes.POINTER(Pages)), ("K_out", ctypes.c_void_p), ("V_out", ctypes.c_void_p),
+                ("mass_out", ctypes.c_void_p), ("out_len", ctypes.c_int32), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p)]
 
 
 _lib = None
@@ -100,6 +133,16 @@ def lib():
         L.sik_decode_step_q2.restype = ctypes.c_int
         L.sik_decode_step_q2.argtypes = [lp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, f32, vp, vp, vp, sz, vp,
                                          ctypes.POINTER(ctypes.c_float)]
+        L.sik_rope_append.restype = ctypes.c_int
+        L.sik_rope_append.argtypes = [lp, ctypes.POINTER(Chunk), ctypes.POINTER(RopeArgs)]
+        L.sik_chunk_workspace_bytes.restype = sz
+        L.sik_chunk_workspace_bytes.argtypes = [lp, i32]
+        L.sik_chunk_attn.restype = ctypes.c_int
+        L.sik_chunk_attn.argtypes = [lp, ctypes.POINTER(Chunk), vp, vp, vp, f32, vp, vp, vp, sz, vp]
+        L.sik_attn_mass.restype = ctypes.c_int
+        L.sik_attn_mass.argtypes = [lp, ctypes.POINTER(Chunk), vp, vp, f32, vp, i32, vp, vp, vp]
+        L.sik_evict.restype = ctypes.c_int
+        L.sik_evict.argtypes = [lp, ctypes.POINTER(EvictArgs)]
         _lib = L
     return _lib
 
@@ -280,3 +323,166 @@ def sik_decode_step_profiled(layout, q, k_new, v_new, K, V, seq_len, mu, codeboo
                                           float(softmax_scale), _ptr(out), _ptr(idx_out), _ptr(workspace),
                                           workspace.numel() if workspace is not None else 0, _stream(), us))
     return list(us)
+
+
+# ---- the prompt side of the cache.  These calls check types, shapes and devices of the tensors here; what the C ABI can
+# see (alignment, ranges, page sizes) it checks itself.
+
+def _tensor(name, t, dtype, shape=None, numel=None, optional=False):
+    """Address of a tensor after its checks, None for an absent optional one."""
+    if t is None:
+        if optional:
+            return None
+        raise ValueError(f"{name} is required")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: {t.dtype} given, {dtype} needed")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)} given, {shape} needed")
+    if numel is not None and t.numel() != numel:
+        raise ValueError(f"{name}: {t.numel()} elements given, {numel} needed")
+    _on_device(name, t)
+    return t.data_ptr()
+
+
+def _on_device(name, t):
+    if torch.cuda.is_available() and t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the call runs on cuda:{torch.cuda.current_device()}")
+
+
+_SIK2TORCH = {SIK_F16: torch.float16, SIK_BF16: torch.bfloat16, SIK_F32: torch.float32}
+
+
+def make_pages(page_table, page_len, n_pages) -> Pages:
+    """Description of a paged cache: page_table [B, pages_per_seq] int32, pools of n_pages pages of page_len tokens."""
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [batch, pages per sequence]")
+    pages = Pages(_tensor("page_table", page_table, torch.int32), page_table.shape[1], int(page_len), int(n_pages))
+    pages.tensor = page_table
+    return pages
+
+
+def make_chunk(n, seq_len, n_new=None, pages=None) -> Chunk:
+    """A chunk of n new tokens per sequence (n_new[b] of them real) behind the seq_len[b] tokens in the cache."""
+    chunk = Chunk(int(n), _tensor("n_new", n_new, torch.int32, optional=True), _tensor("seq_len", seq_len, torch.int32),
+                  None if pages is None else ctypes.pointer(pages))
+    chunk.tensors = (seq_len, n_new, pages)
+    return chunk
+
+
+def _check_chunk(layout, chunk):
+    seq_len, n_new, pages = chunk.tensors
+    if seq_len.numel() != layout.batch or (n_new is not None and n_new.numel() != layout.batch):
+        raise ValueError("seq_len and n_new hold one length per sequence")
+    _check_page_table(layout, pages)
+    return pages
+
+
+def _check_page_table(layout, pages):
+    if pages is not None and pages.tensor.shape[0] != layout.batch:
+        raise ValueError("page_table holds one row per sequence")
+
+
+def _cache(name, t, layout, pages, optional=False):
+    """Address of one side of a contiguous or paged cache."""
+    if pages is None:
+        shape = (layout.batch, layout.n_kv_heads, layout.max_len, layout.head_dim)
+    else:
+        shape = (pages.n_pages, layout.n_kv_heads, pages.page_len, layout.head_dim)
+    return _tensor(name, t, _SIK2TORCH[layout.kv_dtype], shape, optional=optional)
+
+
+def _head_rows(name, t, layout, n, heads):
+    """Address and token stride of [B, n, heads, D] head rows, which may be part of a wider projection's output."""
+    if t.dtype != _SIK2TORCH[layout.kv_dtype] or tuple(t.shape) != (layout.batch, n, heads, layout.head_dim):
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} given, {_SIK2TORCH[layout.kv_dtype]} "
+                         f"{(layout.batch, n, heads, layout.head_dim)} needed")
+    D = layout.head_dim
+    stride = t.stride(1) if n > 1 else t.stride(0) if layout.batch > 1 else heads * D
+    if t.stride(3) != 1 or (heads > 1 and t.stride(2) != D) or (layout.batch > 1 and t.stride(0) != n * stride):
+        raise ValueError(f"{name}: head rows of a token must be contiguous and tokens evenly spaced")
+    _on_device(name, t)
+    return t.data_ptr(), stride
+
+
+def sik_rope_append(layout, chunk, q, k, q_out, *, v=None, k_out=None, K=None, V=None, q_weight=None, k_weight=None,
+                    eps=1e-6, inv_freq=None, interleaved=False, positions=None):
+    """Per-head norms and position rotation of q, k [B,n,heads,D]; keys (and values) into the cache, or keys to k_out."""
+    B, n, D = layout.batch, chunk.n, layout.head_dim
+    kd = _SIK2TORCH[layout.kv_dtype]
+    pages = _check_chunk(layout, chunk)
+    qp, qs = _head_rows("q", q, layout, n, layout.n_q_heads)
+    kp, ks = _head_rows("k", k, layout, n, layout.n_kv_heads)
+    vp, vs = (None, 0) if v is None else _head_rows("v", v, layout, n, layout.n_kv_heads)
+    st = _stream()
+    a = RopeArgs(qp, kp, vp, qs, ks, vs, _tensor("q_weight", q_weight, torch.float32, (D,), optional=True),
+                 _tensor("k_weight", k_weight, torch.float32, (D,), optional=True), float(eps),
+                 _tensor("inv_freq", inv_freq, torch.float32, optional=True),
+                 0 if inv_freq is None else 2 * inv_freq.numel(), 1 if interleaved else 0,
+                 _tensor("positions", positions, torch.int32, (B, n), optional=True),
+                 _tensor("q_out", q_out, kd, (B, n, layout.n_q_heads, D)),
+                 _tensor("k_out", k_out, kd, (B, n, layout.n_kv_heads, D), optional=True),
+                 _cache("K", K, layout, pages, optional=True), _cache("V", V, layout, pages, optional=True),
+                 None if st is None else st.value)
+    _check(lib().sik_rope_append(ctypes.byref(layout), ctypes.byref(chunk), ctypes.byref(a)))
+
+
+def sik_chunk_workspace_bytes(layout: Layout, n: int) -> int:
+    return int(lib().sik_chunk_workspace_bytes(ctypes.byref(layout), int(n)))
+
+
+def alloc_chunk_workspace(layout: Layout, n: int, device="cuda") -> torch.Tensor:
+    """Scratch memory of sik_chunk_attn and sik_evict for chunks of up to n tokens (needs no initialisation)."""
+    size = sik_chunk_workspace_bytes(layout, n)
+    if size == 0:
+        raise SikError(-2, "sik_chunk_workspace_bytes rejected the layout / n")
+    return torch.empty(size, dtype=torch.uint8, device=device)
+
+
+def _scratch(workspace):
+    return None if workspace is None else _tensor("workspace", workspace, torch.uint8)
+
+
+def sik_chunk_attn(layout, chunk, q, K, V, softmax_scale, out, lse, workspace):
+    """Attention of the chunk's queries q [B,n,Hq,D] over the cache; lse [B,n,Hq] fp32 or None."""
+    rows = (layout.batch, chunk.n, layout.n_q_heads)
+    pages = _check_chunk(layout, chunk)
+    _check(lib().sik_chunk_attn(
+        ctypes.byref(layout), ctypes.byref(chunk), _tensor("q", q, _SIK2TORCH[layout.kv_dtype], (*rows, layout.head_dim)),
+        _cache("K", K, layout, pages), _cache("V", V, layout, pages), float(softmax_scale),
+        _tensor("out", out, _SIK2TORCH[layout.out_dtype], (*rows, layout.head_dim)),
+        _tensor("lse", lse, torch.float32, rows, optional=True), _scratch(workspace),
+        workspace.numel() if workspace is not None else 0, _stream()))
+
+
+def sik_attn_mass(layout, chunk, q, K, softmax_scale, lse, n_obs, before, mass):
+    """Attention weight of the cached tokens from the last n_obs queries; before [B,Hkv,max_len] fp32 or None is added."""
+    rows = (layout.batch, chunk.n, layout.n_q_heads)
+    sums = (layout.batch, layout.n_kv_heads, layout.max_len)
+    pages = _check_chunk(layout, chunk)
+    _check(lib().sik_attn_mass(
+        ctypes.byref(layout), ctypes.byref(chunk), _tensor("q", q, _SIK2TORCH[layout.kv_dtype], (*rows, layout.head_dim)),
+        _cache("K", K, layout, pages), float(softmax_scale), _tensor("lse", lse, torch.float32, rows), int(n_obs),
+        _tensor("before", before, torch.float32, sums, optional=True), _tensor("mass", mass, torch.float32, sums),
+        _stream()))
+
+
+def sik_evict(layout, mass, seq_len, n_keep, keep, workspace, *, n_sink=0, n_recent=0, new_len=None, K=None, V=None,
+              pages=None, K_out=None, V_out=None, mass_out=None):
+    """The n_keep tokens per (sequence, KV head) that stay, and with K_out and V_out the cache cut down to them."""
+    B, H, D = layout.batch, layout.n_kv_heads, layout.head_dim
+    _check_page_table(layout, pages)
+    out_len = K_out.shape[2] if K_out is not None else mass_out.shape[2] if mass_out is not None else 0
+    kd, st = _SIK2TORCH[layout.kv_dtype], _stream()
+    a = EvictArgs(_tensor("mass", mass, torch.float32, (B, H, layout.max_len)),
+                  _tensor("seq_len", seq_len, torch.int32, numel=B), int(n_keep), int(n_sink), int(n_recent),
+                  _tensor("keep", keep, torch.int32, (B, H, int(n_keep))),
+                  _tensor("new_len", new_len, torch.int32, numel=B, optional=True),
+                  _cache("K", K, layout, pages, optional=True), _cache("V", V, layout, pages, optional=True),
+                  None if pages is None else ctypes.pointer(pages),
+                  _tensor("K_out", K_out, kd, (B, H, out_len, D), optional=True),
+                  _tensor("V_out", V_out, kd, (B, H, out_len, D), optional=True),
+                  _tensor("mass_out", mass_out, torch.float32, (B, H, out_len), optional=True), out_len,
+                  _scratch(workspace), workspace.numel() if workspace is not None else 0, None if st is None else st.value)
+    _check(lib().sik_evict(ctypes.byref(layout), ctypes.byref(a)))

@@ -33,7 +33,7 @@ static void* static_scratch() {
 
 static size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
-static int check_layout(const sik_layout* l, Dims* d) {
+int check_layout(const sik_layout* l, Dims* d) {
     if (!l) return SIK_ERR_NULL;
     if (l->batch < 1 || l->n_kv_heads < 1 || l->n_q_heads < 1 || l->max_len < 1) return SIK_ERR_SHAPE;
     if (l->head_dim != kD) return SIK_ERR_SHAPE;
@@ -124,6 +124,7 @@ const char* sik_strerror(int status) {
         case SIK_ERR_STATIC_LIMIT:
             return "sik_decode_step_static: this layout / k needs more scratch memory than the library's built-in "
                    "buffer (SIK_STATIC_SCRATCH_BYTES); use sik_decode_step with a workspace";
+        case SIK_ERR_ALIGN: return "a pointer or stride is not 16-byte aligned";
         default: return "unknown status";
     }
 }

@@ -86,6 +86,7 @@ inline bool gather_streams(const Dims& d, int k) {
     return static_cast<int64_t>(d.rows()) * k * 512 >= (64ll << 20);
 }
 
+int check_layout(const sik_layout* l, Dims* d);  // sik_status; fills d
 Workspace carve(const Dims& d, int k, void* base);
 
 // launchers (return hipError_t of the launch)

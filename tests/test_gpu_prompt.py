@@ -1,0 +1,512 @@
+"""The prompt side of the cache on the GPU: norms with rotation, chunk attention, attention weights, eviction, against their
+formulas in 64 bits; then the calls one after the other as a serving program makes them."""
+import math
+
+import pytest
+import torch
+
+import paper_2603_14224_amd as sik
+from prompt_reference import (D, SCALE, attn64, gather_cache, keep64, lse_tolerance, mass64, out_tolerance, rope64,
+                              rope_tolerance)
+
+pytestmark = pytest.mark.gpu
+BF, FP = torch.bfloat16, torch.float16
+
+
+def gen_of(*seed):
+    return torch.Generator(device="cuda").manual_seed(abs(hash(seed)) % (1 << 31))
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def randn(shape, gen, dtype, scale=1.0):
+    return (torch.randn(shape, generator=gen, device="cuda") * scale).to(dtype)
+
+
+class Cache:
+    """A contiguous or paged cache of random rows; whatever belongs to no token of a sequence is NaN."""
+
+    def __init__(self, B, Hkv, cap, dtype, page, lengths, gen, holes=()):
+        self.page, self.pages, self.table, self.lengths = page, None, None, lengths
+        if page:
+            per = (cap + page - 1) // page
+            n_pages = B * per + 2
+            self.table = torch.randperm(n_pages, generator=gen, device="cuda")[:B * per].view(B, per).int()
+            for b, p, value in holes:
+                self.table[b, p] = value
+            shape = (n_pages, Hkv, page, D)
+            self.pages = sik.make_pages(self.table, page, n_pages)
+        else:
+            shape = (B, Hkv, cap, D)
+        self.K = torch.full(shape, float("nan"), dtype=dtype, device="cuda")
+        self.V = torch.full(shape, float("nan"), dtype=dtype, device="cuda")
+        for b, length in enumerate(lengths):
+            for x in (self.K, self.V):
+                rows = randn((Hkv, length, D), gen, dtype) * torch.exp(0.5 * torch.randn(D, generator=gen, device="cuda")).to(dtype)
+                self.write(x, b, 0, rows)
+
+    def write(self, x, b, at, rows):
+        j = torch.arange(at, at + rows.shape[1], device="cuda")
+        if self.table is None:
+            x[b, :, j] = rows
+        else:
+            pg = self.table[b].long()[j // self.page]
+            ok = (pg >= 0) & (pg < x.shape[0])
+            x[pg[ok], :, (j % self.page)[ok]] = rows[:, ok].transpose(0, 1)
+
+    def rows(self, x, b, length):
+        return gather_cache(x, self.table, b, length)
+
+
+# --------------------------------------------------------------------------------------------- norms and rotation
+
+ROPE = [
+    # B, Hkv, Hq, n, past, n_new, page, dtype, rotary, interleaved, norm, fused, rows
+    (1, 8, 32, 1, [0], None, 0, BF, 128, False, True, True, True),
+    (1, 1, 4, 1, [4_000_000], None, 0, BF, 128, False, True, False, True),
+    (2, 2, 6, 5, [7, 0], [5, 0], 0, FP, 128, False, True, True, False),
+    (3, 1, 12, 33, [100, 0, 31], [33, 1, 17], 16, BF, 64, False, False, False, False),
+    (2, 2, 2, 70, [3, 64], None, 32, FP, 96, False, True, True, False),
+    (2, 3, 9, 40, [11, 5], [40, 39], 0, BF, 32, True, True, True, False),
+    (1, 2, 10, 130, [62], None, 64, FP, 128, True, False, False, False),
+    (2, 8, 40, 3, [9, 2], None, 0, BF, 0, False, True, True, True),
+    (1, 8, 64, 600, [1000], None, 128, BF, 16, False, True, True, False),
+]
+
+
+@pytest.mark.parametrize("B,Hkv,Hq,n,past,n_new,page,dtype,rotary,interleaved,norm,fused,rows", ROPE)
+def test_rope_append(B, Hkv, Hq, n, past, n_new, page, dtype, rotary, interleaved, norm, fused, rows):
+    gen = gen_of(B, Hq, n, rotary)
+    new = n_new or [n] * B
+    cap = max(p + n for p in past) + 3 if not rows else max(past) + n
+    if fused:
+        qkv = randn((B, n, (Hq + 2 * Hkv) * D), gen, dtype)
+        q = qkv[:, :, :Hq * D].unflatten(2, (Hq, D))
+        k = qkv[:, :, Hq * D:(Hq + Hkv) * D].unflatten(2, (Hkv, D))
+        v = qkv[:, :, (Hq + Hkv) * D:].unflatten(2, (Hkv, D))
+    else:
+        q, k, v = (randn((B, n, h, D), gen, dtype) for h in (Hq, Hkv, Hkv))
+    qw, kw = (1 + 0.2 * torch.randn(D, generator=gen, device="cuda") for _ in range(2)) if norm else (None, None)
+    freq = (500000.0 ** (-torch.arange(0, rotary, 2, device="cuda").double() / max(rotary, 1))).float() if rotary else None
+    lay = sik.make_layout(B, Hkv, Hq, D, cap, dtype)
+    q_out = torch.full((B, n, Hq, D), 7.0, dtype=dtype, device="cuda")
+    ch = dict(n_new=None if n_new is None else ints(n_new))
+    if rows:
+        k_out = torch.full((B, n, Hkv, D), 7.0, dtype=dtype, device="cuda")
+        chunk = sik.make_chunk(n, ints(past), **ch)
+        sik.sik_rope_append(lay, chunk, q, k, q_out, k_out=k_out, q_weight=qw, k_weight=kw, eps=1e-5, inv_freq=freq,
+                            interleaved=interleaved)
+    else:
+        c = Cache(B, Hkv, cap, dtype, page, past, gen)
+        K0, V0 = c.K.clone(), c.V.clone()
+        chunk = sik.make_chunk(n, ints(past), pages=c.pages, **ch)
+        sik.sik_rope_append(lay, chunk, q, k, q_out, v=v, K=c.K, V=c.V, q_weight=qw, k_weight=kw, eps=1e-5, inv_freq=freq,
+                            interleaved=interleaved)
+    for b in range(B):
+        m = new[b]
+        pos = torch.arange(past[b], past[b] + m, device="cuda")
+        assert (q_out[b, m:] == 7).all()
+        for got, x, w in ((q_out[b, :m], q[b, :m], qw),
+                          (k_out[b, :m] if rows else c.rows(c.K, b, past[b] + m)[0][:, past[b]:].transpose(0, 1), k[b, :m], kw)):
+            ref, size = rope64(x, w, 1e-5, pos, freq, interleaved)
+            assert ((got.double() - ref).abs() <= rope_tolerance(ref, size, dtype)).all()
+        if not rows:
+            assert torch.equal(c.rows(c.V, b, past[b] + m)[0][:, past[b]:], v[b, :m].transpose(0, 1))
+            c.write(K0, b, past[b], c.rows(c.K, b, past[b] + m)[0][:, past[b]:])
+            c.write(V0, b, past[b], v[b, :m].transpose(0, 1))
+    if not rows:  # nothing else of the cache changed
+        assert torch.equal(c.K.view(torch.int16), K0.view(torch.int16)) and torch.equal(c.V.view(torch.int16), V0.view(torch.int16))
+
+
+def test_rope_positions_holes_and_capacity():
+    gen = gen_of(5)
+    B, Hkv, Hq, n, cap = 2, 2, 4, 20, 48
+    c = Cache(B, Hkv, cap, BF, 16, [10, 40], gen, holes=[(0, 1, -1), (1, 2, 99)])
+    K0 = c.K.clone()
+    q, k, v = (randn((B, n, h, D), gen, BF) for h in (Hq, Hkv, Hkv))
+    freq = (10000.0 ** (-torch.arange(0, D, 2, device="cuda").double() / D)).float()
+    pos = torch.randint(-50, 1 << 30, (B, n), generator=gen, device="cuda").int()
+    q_out = torch.full((B, n, Hq, D), 7.0, dtype=BF, device="cuda")
+    lay = sik.make_layout(B, Hkv, Hq, D, cap, BF)
+    sik.sik_rope_append(lay, sik.make_chunk(n, ints([10, 40]), pages=c.pages), q, k, q_out, v=v, K=c.K, V=c.V, inv_freq=freq,
+                        positions=pos)
+    for b, fit in ((0, 20), (1, 8)):  # the second sequence has room for eight tokens
+        ref, size = rope64(q[b, :fit], None, 0, pos[b, :fit], freq, False)
+        # a position above 2^29 times a frequency is rounded in 64 bits, as is the reference: 2^30 * 2^-53 * 4 radians
+        tol = rope_tolerance(ref, size, BF) + size * 2 ** -21
+        assert ((q_out[b, :fit].double() - ref).abs() <= tol).all()
+        assert (q_out[b, fit:] == 7).all()
+    # sequence 0: tokens 10..15 and, on its third page, none (30 tokens end on the unmapped second); sequence 1: page 2 is
+    # out of the pool, rows 40..47 go nowhere
+    changed = (c.K.view(torch.int16) != K0.view(torch.int16)).any(-1).any(1)
+    want = torch.zeros_like(changed)
+    want[c.table[0, 0].long(), 10:16] = True
+    assert torch.equal(changed, want)
+
+
+# --------------------------------------------------------------------------------------------- chunk attention
+
+CHUNK = [
+    # B, Hkv, Hq, n, past, n_new, page, dtype, out
+    (1, 1, 1, 1, [0], None, 0, BF, BF),
+    (1, 8, 32, 1, [0], None, 0, BF, torch.float32),
+    (2, 2, 6, 1, [62, 500], None, 0, FP, FP),
+    (3, 2, 8, 1, [63, 64, 2000], [1, 0, 1], 16, BF, BF),
+    (1, 1, 40, 1, [1000], None, 0, FP, torch.float32),
+    (1, 2, 8, 17, [31], None, 32, BF, torch.float32),
+    (4, 1, 4, 65, [0, 1, 200, 777], [65, 64, 1, 33], 0, FP, FP),
+    (2, 2, 14, 100, [129, 3], None, 64, BF, BF),
+    (1, 2, 2, 300, [0], None, 0, BF, BF),
+    (1, 1, 5, 333, [90], None, 16, FP, torch.float32),
+    (2, 1, 8, 512, [0, 1000], [512, 511], 128, BF, BF),
+    (1, 1, 4, 1025, [3000], None, 0, FP, FP),
+    (1, 4, 4, 40, [9000], None, 0, BF, BF),
+    (1, 1, 100, 3, [257], None, 0, BF, BF),
+    (2, 1, 3, 7, [5000, 12], None, 1024, FP, torch.float32),
+]
+
+
+def run_chunk(lay, c, q, past, n_new, n, lse=True, ws=None, scale=0.0):
+    out = torch.full(q.shape, 7.0, dtype={0: FP, 1: BF, 2: torch.float32}[lay.out_dtype], device="cuda")
+    l = torch.full(q.shape[:3], 7.0, device="cuda") if lse else None
+    chunk = sik.make_chunk(n, ints(past), n_new=None if n_new is None else ints(n_new), pages=c.pages)
+    sik.sik_chunk_attn(lay, chunk, q, c.K, c.V, scale, out, l, sik.alloc_chunk_workspace(lay, n) if ws is None else ws)
+    return out, l
+
+
+def check_chunk(c, q, past, new, out, lse, scale=SCALE, n_rows=None):
+    for b in range(q.shape[0]):
+        m = new[b]
+        assert (out[b, m:] == 7).all() and (lse is None or (lse[b, m:] == 7).all())
+        if m == 0:
+            continue
+        k, there = c.rows(c.K, b, past[b] + m)
+        v, _ = c.rows(c.V, b, past[b] + m)
+        r = attn64(q[b, :m], k, v, there, past[b], scale)
+        bad = (out[b, :m].double() - r["out"]).abs() / out_tolerance(r, q.dtype, out.dtype, v.double().abs().max())
+        assert not torch.isnan(out[b, :m]).any() and bad.max() <= 1, (b, float(bad.max()))
+        if lse is not None:
+            empty = r["lse"] == -math.inf
+            assert torch.equal(lse[b, :m] == -math.inf, empty) and (out[b, :m][empty] == 0).all()
+            off = (lse[b, :m].double() - r["lse"]).abs()[~empty] / lse_tolerance(r)[~empty]
+            assert off.numel() == 0 or off.max() <= 1, (b, float(off.max()))
+
+
+@pytest.mark.parametrize("B,Hkv,Hq,n,past,n_new,page,dtype,out_dtype", CHUNK)
+def test_chunk_attn(B, Hkv, Hq, n, past, n_new, page, dtype, out_dtype):
+    gen = gen_of(B, Hq, n, page)
+    new = n_new or [n] * B
+    cap = max(p + n for p in past) + 5
+    c = Cache(B, Hkv, cap, dtype, page, [p + m for p, m in zip(past, new)], gen)
+    q = randn((B, n, Hq, D), gen, dtype)
+    lay = sik.make_layout(B, Hkv, Hq, D, cap, dtype, out_dtype)
+    out, lse = run_chunk(lay, c, q, past, n_new, n)
+    check_chunk(c, q, past, new, out, lse)
+    again, _ = run_chunk(lay, c, q, past, n_new, n, lse=False)
+    assert torch.equal(out.view(torch.int16), again.view(torch.int16))  # the same bits with and without lse, run after run
+
+
+@pytest.mark.parametrize("n,past", [(1, 300), (5, 90), (150, 200), (200, 0)])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_chunk_attn_unmapped_pages(n, past, dtype):
+    # holes at the start (rows without any token), in the middle and at the end, negative and beyond the pool
+    gen = gen_of(n, past)
+    B, Hkv, Hq, page = 2, 2, 8, 16
+    holes = [(0, 0, -1), (0, 3, 1 << 30), (0, 4, -7), (1, (past + n - 1) // page, -1)] + [(1, p, -1) for p in range(0, 6)]
+    c = Cache(B, Hkv, past + n, dtype, page, [past + n] * B, gen, holes=holes)
+    q = randn((B, n, Hq, D), gen, dtype)
+    lay = sik.make_layout(B, Hkv, Hq, D, past + n, dtype, torch.float32)
+    out, lse = run_chunk(lay, c, q, [past] * B, None, n)
+    check_chunk(c, q, [past] * B, [n] * B, out, lse)
+
+
+@pytest.mark.parametrize("n", [1, 3, 260])
+def test_chunk_attn_large_and_growing_logits(n):
+    # logits up to several hundred, and keys whose logits grow along the cache, so that the running maximum moves all the time
+    gen = gen_of(n)
+    past, Hkv, Hq = 700, 1, 4
+    c = Cache(1, Hkv, past + n, BF, 0, [past + n], gen)
+    c.K[0, 0] = (c.K[0, 0].float() * torch.linspace(0.1, 30, past + n, device="cuda")[:, None]).to(BF)
+    q = randn((1, n, Hq, D), gen, BF)
+    q[:, :, 1] = 0
+    q[:, :, 2] = c.K[0, 0, -1]
+    lay = sik.make_layout(1, Hkv, Hq, D, past + n, BF, torch.float32)
+    out, lse = run_chunk(lay, c, q, [past], None, n)
+    check_chunk(c, q, [past], [n], out, lse)
+    out, lse = run_chunk(lay, c, q, [past], None, n, scale=0.01)
+    check_chunk(c, q, [past], [n], out, lse, scale=0.01)
+
+
+def test_chunk_attn_lengths_are_clamped():
+    gen = gen_of(77)
+    c = Cache(3, 1, 64, BF, 0, [64, 64, 64], gen)
+    q = randn((3, 10, 2, D), gen, BF)
+    lay = sik.make_layout(3, 1, 2, D, 64, BF)
+    # a negative length counts as none, one beyond the capacity leaves no room, more tokens than the chunk has are the chunk's
+    out, lse = run_chunk(lay, c, q, [-5, 900, 58], [99, 10, 10], 10)
+    check_chunk(c, q, [0, 64, 58], [10, 0, 6], out, lse)
+
+
+def test_chunk_attn_beyond_32_bit_offsets():
+    # a cache of more than 4 GiB a side: the last sequence's rows lie past 2^31 elements
+    B, Hkv, cap = 3, 8, 262144 * 3
+    c = Cache(1, 1, 16, BF, 0, [1], gen_of(1))
+    c.page, c.table, c.pages = 0, None, None
+    c.K = torch.zeros(B, Hkv, cap, D, dtype=BF, device="cuda")
+    c.V = torch.zeros(B, Hkv, cap, D, dtype=BF, device="cuda")
+    gen = gen_of(2)
+    past = cap - 2000
+    for x in (c.K, c.V):
+        x[2, :, :300] = randn((Hkv, 300, D), gen, BF)
+        x[2, :, past - 100:past + 20] = randn((Hkv, 120, D), gen, BF)
+    q = randn((B, 20, Hkv, D), gen, BF) * 4
+    lay = sik.make_layout(B, Hkv, Hkv, D, cap, BF, torch.float32)
+    out, lse = run_chunk(lay, c, q, [0, 5, past], [1, 2, 20], 20)
+    # all rows that are zero have the logit 0: their number goes into the sum, the rest is a small softmax
+    rows = torch.cat([torch.arange(300), torch.arange(past - 100, past + 20)]).cuda()
+    k, v = c.K[2][:, rows].double(), c.V[2][:, rows].double()
+    for h in range(Hkv):
+        z = q[2, :, h].double() @ k[h].T * SCALE
+        z = z.masked_fill(rows[None] > past + torch.arange(20, device="cuda")[:, None], -math.inf)
+        m = z.amax(-1, keepdim=True).clamp(min=0)
+        p = torch.exp(z - m)
+        l = p.sum(-1, keepdim=True) + (past - 400) * torch.exp(-m)
+        ref = (p @ v[h]) / l
+        # logits of |q| |k| up to 4 * 128: 132 * 2^-23 * 512 * SCALE each way; sums of 800K terms of like size in binary32,
+        # split over many partial sums of at most 2^13 steps
+        rel = 2 * 132 * 2 ** -23 * 512 * SCALE * 4 + 2 ** 13 * 2 ** -23
+        spread = (p @ v[h].abs()) / l
+        assert ((out[2, :, h].double() - ref).abs() <= spread * rel + 1e-9).all()
+        assert ((lse[2, :, h].double() - (m + l.log())[:, 0]).abs() <= rel).all()
+
+
+# --------------------------------------------------------------------------------------------- weights of the cached tokens
+
+MASS = [
+    # B, Hkv, Hq, n, past, n_new, page, dtype, n_obs, before
+    (1, 1, 1, 1, [0], None, 0, BF, 1, False),
+    (2, 2, 8, 1, [100, 3000], None, 16, FP, 1, True),
+    (1, 8, 32, 64, [500], None, 0, BF, 64, False),
+    (3, 2, 10, 50, [0, 129, 1000], [50, 7, 0], 32, BF, 20, True),
+    (1, 1, 7, 200, [63], None, 0, FP, 33, False),
+    (1, 2, 16, 300, [0], None, 64, BF, 300, False),
+    (2, 1, 100, 5, [700, 2], None, 0, FP, 3, True),
+]
+
+
+@pytest.mark.parametrize("B,Hkv,Hq,n,past,n_new,page,dtype,n_obs,before", MASS)
+def test_attn_mass(B, Hkv, Hq, n, past, n_new, page, dtype, n_obs, before):
+    gen = gen_of(B, Hq, n, n_obs)
+    new = n_new or [n] * B
+    cap = max(p + n for p in past) + 5
+    holes = [(0, 1, -1)] if page and past[0] + new[0] > 2 * page else []
+    c = Cache(B, Hkv, cap, dtype, page, [p + m for p, m in zip(past, new)], gen, holes=holes)
+    q = randn((B, n, Hq, D), gen, dtype)
+    lay = sik.make_layout(B, Hkv, Hq, D, cap, dtype, torch.float32)
+    _, lse = run_chunk(lay, c, q, past, n_new, n)
+    lse[0, new[0] - 1, 0] = -math.inf  # a query without tokens gives nothing
+    old = torch.rand(B, Hkv, cap, generator=gen, device="cuda")
+    mass = torch.full((B, Hkv, cap), 7.0, device="cuda")
+    chunk = sik.make_chunk(n, ints(past), n_new=None if n_new is None else ints(n_new), pages=c.pages)
+    sik.sik_attn_mass(lay, chunk, q, c.K, 0.0, lse, n_obs, old if before else None, mass)
+    for b in range(B):
+        m, L = new[b], past[b] + new[b]
+        assert (mass[b, :, L:] == 7).all()
+        base = old[b, :, :L].double() if before else torch.zeros(Hkv, L, device="cuda").double()
+        if m == 0:
+            assert torch.equal(mass[b, :, :L].double(), base)
+            continue
+        k, there = c.rows(c.K, b, L)
+        r = attn64(q[b, :m], k, None, there, past[b], SCALE)
+        want, tol = mass64(r, lse[b, :m], n_obs)
+        assert ((mass[b, :, :L].double() - base - want).abs() <= tol + (base + want) * 2 ** -23).all()
+    if before:  # in place
+        sik.sik_attn_mass(lay, chunk, q, c.K, 0.0, lse, n_obs, old, old)
+        for b in range(B):
+            assert torch.equal(old[b, :, :past[b] + new[b]], mass[b, :, :past[b] + new[b]])
+
+
+# --------------------------------------------------------------------------------------------- eviction
+
+EVICT = [
+    # B, Hkv, lengths, n_keep, n_sink, n_recent, page, dtype, kind
+    (1, 1, [1], 1, 0, 0, 0, BF, "plain"),
+    (2, 2, [0, 5], 3, 1, 1, 0, BF, "plain"),
+    (3, 2, [700, 64, 63], 64, 0, 0, 16, FP, "plain"),
+    (1, 8, [5000], 64, 0, 0, 0, BF, "zeros"),
+    (2, 4, [4097, 1000], 1000, 4, 64, 0, BF, "equal"),
+    (1, 2, [2500], 2499, 100, 200, 32, BF, "plain"),
+    (2, 1, [3000, 2999], 300, 100, 200, 0, FP, "plain"),
+    (1, 2, [70000], 2048, 4, 1, 0, BF, "steps"),
+    (1, 1, [140001], 5000, 0, 7, 0, FP, "plain"),
+    (1, 3, [9000], 500, 0, 0, 64, FP, "signs"),
+]
+
+
+@pytest.mark.parametrize("B,Hkv,lengths,n_keep,n_sink,n_recent,page,dtype,kind", EVICT)
+def test_evict(B, Hkv, lengths, n_keep, n_sink, n_recent, page, dtype, kind):
+    gen = gen_of(B, n_keep, page)
+    cap = max(max(lengths), n_keep) + 3
+    c = Cache(B, Hkv, cap, dtype, page, lengths, gen, holes=[(0, 2, -1)] if page == 64 else [])
+    mass = torch.exp(2 * torch.randn(B, Hkv, cap, generator=gen, device="cuda"))
+    if kind == "zeros":
+        mass = torch.where(torch.rand(mass.shape, generator=gen, device="cuda") < 0.995, 0.0, mass)
+    elif kind == "equal":
+        mass[:] = 0.25
+    elif kind == "steps":  # many tokens share a weight
+        mass = torch.round(mass * 4) / 4
+    elif kind == "signs":
+        mass = torch.randn(mass.shape, generator=gen, device="cuda").round(decimals=2) + 0.0
+        mass[0, 0, 5], mass[0, 0, 6], mass[0, 1, 7] = math.inf, -math.inf, -0.0
+    for b, L in enumerate(lengths):
+        mass[b, :, L:] = math.nan
+    lay = sik.make_layout(B, Hkv, Hkv, D, cap, dtype)
+    ws = sik.alloc_chunk_workspace(lay, 1)
+    keep = torch.full((B, Hkv, n_keep), -5, dtype=torch.int32, device="cuda")
+    new_len = ints([-1] * B)
+    Ko, Vo = (torch.full((B, Hkv, n_keep + 2, D), 7.0, dtype=dtype, device="cuda") for _ in range(2))
+    mo = torch.full((B, Hkv, n_keep + 2), 7.0, device="cuda")
+    sik.sik_evict(lay, mass, ints(lengths), n_keep, keep, ws, n_sink=n_sink, n_recent=n_recent, new_len=new_len, K=c.K, V=c.V,
+                  pages=c.pages, K_out=Ko, V_out=Vo, mass_out=mo)
+    assert new_len.tolist() == [min(L, n_keep) for L in lengths]
+    for b, L in enumerate(lengths):
+        m = min(L, n_keep)
+        (k, _), (v, _) = c.rows(c.K, b, L), c.rows(c.V, b, L)
+        for h in range(Hkv):
+            want = keep64(mass[b, h, :L], L, n_keep, n_sink, n_recent)
+            assert keep[b, h].tolist() == want + [-1] * (n_keep - m)
+            assert torch.equal(Ko[b, h, :m], k[h, want]) and torch.equal(Vo[b, h, :m], v[h, want])
+            assert torch.equal(mo[b, h, :m], mass[b, h, want])
+        assert (Ko[b, :, m:] == 7).all() and (Vo[b, :, m:] == 7).all() and (mo[b, :, m:] == 7).all()
+    only = torch.full_like(keep, -5)  # the list alone
+    sik.sik_evict(lay, mass, ints(lengths), n_keep, only, ws, n_sink=n_sink, n_recent=n_recent)
+    assert torch.equal(only, keep)
+
+
+# --------------------------------------------------------------------------------------------- together
+
+def serve(stream=None, page=0, dtype=BF):
+    """A prompt in three chunks, its sinks and an eviction by the last queries, the cut cache compressed, one decode step."""
+    gen = gen_of(99)
+    B, Hkv, Hq, cap, n = 2, 2, 8, 480, 150
+    news = [[150, 150], [150, 90], [100, 0]]
+    c = Cache(B, Hkv, cap, dtype, page, [0, 0], gen)
+    for x in (c.K, c.V):
+        x.zero_()
+    lay = sik.make_layout(B, Hkv, Hq, D, cap, dtype, torch.float32)
+    ws = sik.alloc_chunk_workspace(lay, n)
+    freq = (10000.0 ** (-torch.arange(0, D, 2, device="cuda").double() / D)).float()
+    w = 1 + 0.1 * torch.randn(D, generator=gen, device="cuda")
+    past, seq_len = [0, 0], ints([0, 0])
+    mass = torch.zeros(B, Hkv, cap, device="cuda")
+    res = []
+    for new in news:
+        qkv = randn((B, n, (Hq + 2 * Hkv) * D), gen, dtype)
+        q, k, v = (x.unflatten(2, (-1, D)) for x in qkv.split([Hq * D, Hkv * D, Hkv * D], 2))
+        q_rot = torch.full((B, n, Hq, D), 7.0, dtype=dtype, device="cuda")
+        n_new = ints(new)
+        chunk = sik.make_chunk(n, seq_len, n_new=n_new, pages=c.pages)
+        sik.sik_rope_append(lay, chunk, q, k, q_rot, v=v, K=c.K, V=c.V, q_weight=w, k_weight=w, inv_freq=freq)
+        out, lse = torch.full((B, n, Hq, D), 7.0, device="cuda"), torch.full((B, n, Hq), 7.0, device="cuda")
+        sik.sik_chunk_attn(lay, chunk, q_rot, c.K, c.V, 0.0, out, lse, ws)
+        sik.sik_attn_mass(lay, chunk, q_rot, c.K, 0.0, lse, 32, mass, mass)
+        res.append((list(past), new, q_rot, out, lse, mass.clone()))
+        seq_len = seq_len + n_new
+        past = [p + m for p, m in zip(past, new)]
+    n_keep, sinks = 128, ints([[[0] * 8] * Hkv] * B)
+    sik.sik_evict(lay, mass, seq_len, 8, sinks, ws)
+    keep, kept_len = ints([[[0] * n_keep] * Hkv] * B), ints([0, 0])
+    K2, V2 = (torch.zeros(B, Hkv, n_keep + 8, D, dtype=dtype, device="cuda") for _ in range(2))
+    m2 = torch.zeros(B, Hkv, n_keep + 8, device="cuda")
+    sik.sik_evict(lay, mass, seq_len, n_keep, keep, ws, n_sink=4, n_recent=16, new_len=kept_len, K=c.K, V=c.V, pages=c.pages,
+                  K_out=K2, V_out=V2, mass_out=m2)
+    forced = ints([[[0] * 8] * Hkv] * B)
+    lay2 = sik.make_layout(B, Hkv, Hq, D, n_keep + 8, dtype, torch.float32)
+    ws2 = sik.alloc_workspace(lay2, n_keep)
+    sik.sik_evict(lay2, m2, kept_len, 8, forced, sik.alloc_chunk_workspace(lay2, 1))
+    mu, cb = torch.zeros(B, Hkv, D, device="cuda"), torch.zeros(B, Hkv, 32, 16, 4, device="cuda")
+    counts = torch.zeros(B, Hkv, 32, 16, dtype=torch.int32, device="cuda")
+    codes = torch.zeros(B, Hkv, n_keep + 8, 16, dtype=torch.uint8, device="cuda")
+    sik.sik_quantize_keys(lay2, K2, kept_len, 0, 0, sik.SIK_Q_FIT, mu, cb, counts, codes, ws2)
+    qkv = randn((B, 1, (Hq + 2 * Hkv) * D), gen, dtype)
+    q, k, v = (x.unflatten(2, (-1, D)) for x in qkv.split([Hq * D, Hkv * D, Hkv * D], 2))
+    q1, k1 = torch.zeros(B, 1, Hq, D, dtype=dtype, device="cuda"), torch.zeros(B, 1, Hkv, D, dtype=dtype, device="cuda")
+    lay_full = sik.make_layout(B, Hkv, Hq, D, 4096, dtype, torch.float32)
+    sik.sik_rope_append(lay_full, sik.make_chunk(1, seq_len), q, k, q1, k_out=k1, q_weight=w, k_weight=w, inv_freq=freq)
+    final, idx = torch.zeros(B, Hq, D, device="cuda"), ints([[[0] * 64] * Hq] * B)
+    sik.sik_decode_step_ex(lay2, q=q1.view(B, Hq, D), k_new=k1.view(B, Hkv, D), v_new=v.contiguous().view(B, Hkv, D), K=K2,
+                           V=V2, seq_len=kept_len, mu=mu, codebook=cb, codes=codes, k=64, out=final, idx_out=idx,
+                           forced_idx=forced, workspace=ws2)
+    return dict(c=c, res=res, sinks=sinks, keep=keep, K2=K2, V2=V2, kept_len=kept_len, q1=q1, final=final, idx=idx,
+                forced=forced, mass=mass, seq_len=seq_len)
+
+
+@pytest.mark.parametrize("page", [0, 32])
+def test_prompt_to_decode(page):
+    s = serve(page=page)
+    c = s["c"]
+    for past, new, q, out, lse, _ in s["res"]:
+        check_chunk(c, q, past, new, out, lse)
+    lengths = s["seq_len"].tolist()
+    assert lengths == [400, 240] and s["kept_len"].tolist() == [129, 129]
+    for b in range(2):
+        for h in range(2):
+            m = s["mass"][b, h, :lengths[b]]
+            assert s["sinks"][b, h].tolist() == keep64(m, lengths[b], 8, 0, 0)
+            want = keep64(m, lengths[b], 128, 4, 16)
+            assert s["keep"][b, h].tolist() == want
+            assert torch.equal(s["K2"][b, h, :128], c.rows(c.K, b, lengths[b])[0][h, want])
+    # the decode step attends the forced tokens and others, 64 in all: its row is the softmax over its list
+    for b in range(2):
+        for hq in range(8):
+            idx = s["idx"][b, hq].long()
+            assert idx.unique().numel() == 64 and set(s["forced"][b, hq // 4].tolist()) <= set(idx.tolist())
+            z = s["K2"][b, hq // 4, idx].double() @ s["q1"][b, 0, hq].double() * SCALE
+            ref = torch.softmax(z, 0) @ s["V2"][b, hq // 4, idx].double()
+            assert (s["final"][b, hq].double() - ref).abs().max() <= 1e-5 * ref.abs().max()
+
+
+def test_streams_and_graphs():
+    plain = serve()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = serve()
+    side.synchronize()
+    for x in ("final", "K2", "keep", "mass"):
+        assert torch.equal(plain[x], other[x])
+    # captured: a chunk's attention, weights and eviction, two graphs that share a workspace, replayed in turn with work between
+    gen = gen_of(7)
+    graphs, states = [], []
+    lay = sik.make_layout(1, 2, 8, D, 900, BF, torch.float32)
+    ws = sik.alloc_chunk_workspace(lay, 40)
+    for n, past in ((40, 800), (1, 890)):
+        c = Cache(1, 2, 900, BF, 0, [past + n], gen)
+        q = randn((1, n, 8, D), gen, BF)
+        st = dict(c=c, q=q, out=torch.zeros(1, n, 8, D, device="cuda"), lse=torch.zeros(1, n, 8, device="cuda"),
+                  mass=torch.zeros(1, 2, 900, device="cuda"), keep=ints([[[0] * 100] * 2]), len=ints([past]), tot=ints([past + n]))
+
+        def step(st=st, n=n):
+            chunk = sik.make_chunk(n, st["len"])
+            sik.sik_chunk_attn(lay, chunk, st["q"], st["c"].K, st["c"].V, 0.0, st["out"], st["lse"], ws)
+            sik.sik_attn_mass(lay, chunk, st["q"], st["c"].K, 0.0, st["lse"], n, None, st["mass"])
+            sik.sik_evict(lay, st["mass"], st["tot"], 100, st["keep"], ws)
+        step()
+        torch.cuda.synchronize()
+        st["want"] = [st[x].clone() for x in ("out", "lse", "mass", "keep")]
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step()
+        graphs.append(g)
+        states.append(st)
+    for _ in range(4):
+        for g, st in zip(graphs, states):
+            for x in ("out", "lse", "mass", "keep"):
+                st[x].zero_()
+            ws.fill_(0xA5)  # a call expects nothing of what the workspace holds
+            g.replay()
+            torch.cuda.synchronize()
+            for x, w in zip(("out", "lse", "mass", "keep"), st["want"]):
+                assert torch.equal(st[x], w)
