@@ -1,60 +1,488 @@
-// Attention of a chunk of new tokens over a contiguous or paged cache.
+// Attention of a chunk of new tokens over a contiguous or paged cache: one pass over the cache with the running maximum and
+// sum of a softmax, both products on the matrix units.
+//
+// The rows that share a KV head's keys are the chunk's tokens times the R query heads of its group; row m is token m / R,
+// head m % R.  A wavefront holds 32 of them.  Its logits are computed transposed, S^T = K Q^T, so that a lane has one query
+// (column l % 32) and half of the tile's keys in its registers: maximum and sum of a softmax row stay in the lane but for one
+// exchange with the lane 32 away, and the weights are already laid out as the second operand of O^T = V^T P^T, whose first
+// one the transposing LDS reads deliver in the same order of tokens.  Nothing of the weights goes through LDS.
+//
+// Two forms.  `rows`: four wavefronts of a workgroup take 128 rows and share tiles of 64 tokens, loaded into LDS one tile
+// ahead.  `tokens`: few rows (at most 32 per KV head, a generated token above all); each wavefront takes its own tiles of 32
+// tokens, and the four states of a workgroup are joined at the end.  Either form splits the cache over several workgroups
+// where there are too few to fill the chip; a second launch joins their states.
 #include "sik_attn_core.h"
-#include "sik_chunk.h"
+#include "sik_mma.h"
 
 namespace sik {
 
-// A workgroup takes one token of the chunk and a block of up to four query heads of one KV head, and walks over the cache.
-template <int DT, int ODT>
-__global__ __launch_bounds__(kBlock) void chunk_attn_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ K,
-                                                            const uint16_t* __restrict__ V, CacheView cv, ChunkView ch,
-                                                            int Hq, int R, int nblk, float scale_log2e,
-                                                            void* __restrict__ out, float* __restrict__ lse) {
-    constexpr int NH = kSharedHeads;
-    __shared__ MergeLds<NH> lds;
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, p = lane & 15;
-    const int blk = blockIdx.x % nblk, u = blockIdx.x / nblk;
-    const int h = u % cv.Hkv, tok = u / cv.Hkv, b = tok / ch.n, t = tok % ch.n;
-    const int past = chunk_past(ch, b, cv.Lmax);
-    if (t >= chunk_new(ch, b, past, cv.Lmax)) return;
-    const int nh = min(NH, R - blk * NH);
-    const int64_t row0 = static_cast<int64_t>(tok) * Hq + h * R + blk * NH;
-    uint4 qraw[NH];
-    SoftmaxState st[NH];
+constexpr int kRowsTile = 128;   // rows of a workgroup of the `rows` form
+constexpr int kTokensTile = 32;  // of the `tokens` form
+constexpr int kMaxParts = 128;   // workgroups that share one row tile's cache
+// A row's reference maximum moves only when a logit exceeds it by more than this (in powers of two): weights stay below 256
+// and the 64 registers of the output are rescaled a few times per pass instead of once per tile.
+constexpr float kSlack = 8.0f;
+
+struct ChunkAttn {
+    const uint16_t *q, *K, *V;
+    CacheView cv;
+    ChunkView ch;
+    int B, Hq, R, tiles, parts;  // row tiles per unit, workgroups per row tile
+    float scale_log2e;
+    void* out;
+    float* lse;
+    float* part_o;   // [unit][tile][part][rows][kD]
+    float* part_ml;  // [unit][tile][part][rows][2]
+};
+
+// A wavefront's 32 rows: one query per lane (both halves hold the same), output registers [channel block][16].
+struct RowState {
+    float m, l;
+    f32x16 o[4];
+};
+
+__device__ __forceinline__ void init_rows(RowState& st) {
+    st.m = kNegBig;
+    st.l = 0.0f;
 #pragma unroll
-    for (int x = 0; x < NH; ++x) {
-        qraw[x] = x < nh ? reinterpret_cast<const uint4*>(q + (row0 + x) * kD)[p] : make_uint4(0u, 0u, 0u, 0u);
-        init_state(st[x]);
-    }
-    for (int j0 = 0; j0 <= past + t; j0 += 16) {  // 16 tokens lie on one page
-        if (((j0 >> 4) & 3) != wv) continue;
-        const int64_t at = cache_row(cv, b, h, j0);
-        if (at < 0) continue;
-        auto fetch = [&](int j) { return j; };
-        attend_list_multi<DT, NH>(fetch, min(16, past + t + 1 - j0), 0, 16,
-                                  reinterpret_cast<const uint4*>(K + at * kD),
-                                  reinterpret_cast<const uint4*>(V + at * kD), qraw, scale_log2e, 16, st);
-    }
-    workgroup_merge_multi<NH>(st, nh, lds, [&](int x, int d, float M, float l, float o) {
-        store_out<ODT>(out, (row0 + x) * kD + d, l > 0.0f ? o / l : 0.0f);
-        if (lse && d == 0) lse[row0 + x] = l > 0.0f ? (M + log2f(l)) * 0.6931471805599453f : -__builtin_inff();
-    });
+    for (int c = 0; c < 4; ++c) st.o[c] = f32x16{};
 }
 
-size_t chunk_attn_bytes(const Dims&, int) { return 0; }
+// One tile of 32 NK tokens: `keys` and `values` are its LDS rows, s its logits.  PREC (binary32 outputs): what a weight loses
+// in 16 bits is kept as a second weight and a second product.
+template <int DT, int NK>
+__device__ __forceinline__ void tile_logits(const char* keys, int lane, const u32x4 (&qf)[8], f32x16 (&s)[NK]) {
+#pragma unroll
+    for (int t = 0; t < NK; ++t) s[t] = f32x16{};
+#pragma unroll
+    for (int step = 0; step < 8; ++step)
+#pragma unroll
+        for (int t = 0; t < NK; ++t) s[t] = mma32<DT>(row_fragment(keys + t * 32 * 256, lane, step), qf[step], s[t]);
+}
+
+// Logits of tokens beyond `last` (relative to the tile) or of 16-token groups whose bit is not in `mapped` do not count.
+template <int NK>
+__device__ __forceinline__ void mask_logits(f32x16 (&s)[NK], int lane, int last, uint32_t mapped) {
+    const int lim = last - 4 * (lane >> 5);
+#pragma unroll
+    for (int t = 0; t < NK; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int at = 32 * t + 8 * (i / 4) + i % 4;
+            if (at > lim || !((mapped >> (2 * t + i / 8)) & 1u)) s[t][i] = -__builtin_inff();
+        }
+}
+
+template <int DT, int NK, bool PREC>
+__device__ __forceinline__ void tile_update(RowState& st, const f32x16 (&s)[NK], const char* values, int lane, float c) {
+    float top = s[0][0];
+#pragma unroll
+    for (int t = 0; t < NK; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
+    float lo, hi;
+    both_halves(top, lo, hi);
+    top = fmaxf(lo, hi) * c;
+    if (__any(top > st.m + kSlack)) {
+        const float m = fmaxf(st.m, top), f = fast_exp2(st.m - m);
+        st.m = m;
+        st.l *= f;
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) st.o[b][i] *= f;
+    }
+    u32x4 w[2 * NK], rest[PREC ? 2 * NK : 1];
+    float sum = 0.0f;
+#pragma unroll
+    for (int t = 0; t < NK; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+            const float a = fast_exp2(fmaf(s[t][i], c, -st.m)), b = fast_exp2(fmaf(s[t][i + 1], c, -st.m));
+            sum += a;
+            sum += b;
+            const uint32_t p = pack16<DT>(a, b);
+            w[2 * t + i / 8][(i % 8) / 2] = p;
+            if constexpr (PREC)
+                rest[2 * t + i / 8][(i % 8) / 2] = pack16<DT>(a - widen16<DT>(p & 0xffffu), b - widen16<DT>(p >> 16));
+        }
+    st.l += sum;
+#pragma unroll
+    for (int g = 0; g < 2 * NK; ++g)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const u32x4 v = value_fragment(values + g * 16 * 256, lane, b);
+            st.o[b] = mma32<DT>(v, w[g], st.o[b]);
+            if constexpr (PREC) st.o[b] = mma32<DT>(v, rest[g], st.o[b]);
+        }
+}
+
+template <int DT>
+__device__ __forceinline__ void load_queries(const uint16_t* row, int lane, u32x4 (&qf)[8]) {
+#pragma unroll
+    for (int step = 0; step < 8; ++step)
+        qf[step] = *reinterpret_cast<const u32x4*>(row + 16 * step + 8 * (lane >> 5));
+}
+
+template <int ODT>
+__device__ __forceinline__ void store4(void* out, size_t at, float a, float b, float c, float d) {
+    if constexpr (ODT == kF32)
+        *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(a, b, c, d);
+    else
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = make_uint2(pack16<ODT>(a, b), pack16<ODT>(c, d));
+}
+
+__device__ __forceinline__ float log_sum(float m, float l) {
+    return l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : -__builtin_inff();
+}
+
+// A workgroup's place in the launch.  Workgroups go to the XCDs in turn and each XCD has a cache of its own: where the units
+// divide by 8, a unit's workgroups all go to one XCD, so that its keys and values are read into one cache only.  The row
+// tiles with the most tokens in front of them start first.
+struct Place {
+    int unit, tile, part;
+};
+__device__ __forceinline__ Place place_of(int idx, int units, int tiles, int parts) {
+    const int per = tiles * parts;
+    int u, r;
+    if ((units & 7) == 0) {
+        const int k = idx >> 3;
+        u = (k / per) * 8 + (idx & 7);
+        r = k % per;
+    } else {
+        u = idx % units;
+        r = idx / units;
+    }
+    return Place{u, tiles - 1 - r / parts, r % parts};
+}
+
+// 16-token groups of a tile: address of the first row of the group that holds token j (uniform), or nullptr.
+__device__ __forceinline__ const uint16_t* group_row(const uint16_t* x, int64_t row) {
+    return row < 0 ? nullptr : uniform(x + row * kD);
+}
+
+template <int DT, int ODT, bool PAGED>
+__global__ __launch_bounds__(kBlock, 2) void chunk_rows_kernel(const ChunkAttn a) {
+    constexpr int kTile = 64, kSide = kTile * 256, kBuf = 2 * kSide;
+    __shared__ struct {
+        __align__(16) char tiles[2 * kBuf];  // first: the loads reach the first 64 KB
+        int mapped[2][4];
+    } shared;
+    char* lds = shared.tiles;
+    auto& s_mapped = shared.mapped;
+    const int lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
+    const Place pl = place_of(blockIdx.x, a.B * a.cv.Hkv, a.tiles, a.parts);
+    const int b = pl.unit / a.cv.Hkv, h = pl.unit % a.cv.Hkv;
+    const int past = chunk_past(a.ch, b, a.cv.Lmax), nn = chunk_new(a.ch, b, past, a.cv.Lmax);
+    const int rows = nn * a.R, r0 = pl.tile * kRowsTile;
+    if (r0 >= rows) return;
+    const int end = past + (min(r0 + kRowsTile, rows) - 1) / a.R + 1;  // tokens that the last row attends
+    const int n_tiles = (end + kTile - 1) / kTile;
+    const int t0 = static_cast<int>(static_cast<int64_t>(n_tiles) * pl.part / a.parts);
+    const int t1 = static_cast<int>(static_cast<int64_t>(n_tiles) * (pl.part + 1) / a.parts);
+
+    const int w0 = r0 + 32 * wv;                       // this wavefront's rows
+    const int mine = min(w0 + (lane & 31), rows - 1);  // this lane's row (the last one again beyond the end)
+    const int t = mine / a.R;
+    const int64_t qrow = (static_cast<int64_t>(b) * a.ch.n + t) * a.Hq + h * a.R + mine % a.R;
+    const int first_t = uniform(min(w0, rows - 1) / a.R), last_t = uniform(min(w0 + 31, rows - 1) / a.R);
+    u32x4 qf[8];
+    load_queries<DT>(a.q + qrow * kD, lane, qf);
+    RowState st;
+    init_rows(st);
+
+    const RowOffsets ko = row_offsets<true>(lane, 15), vo = row_offsets<false>(lane, 15);
+    auto issue = [&](int tile, int buf) {
+        int g = tile * kTile + 16 * wv;
+        if (g >= end) g = (end - 1) & ~15;
+        const int64_t row = cache_row(a.cv, b, h, g);
+        const uint16_t *kb = group_row(a.K, row), *vb = group_row(a.V, row);
+        if constexpr (PAGED) {
+            if (lane == 0) s_mapped[buf][wv] = kb != nullptr;
+        }
+        const uint32_t to = buf * kBuf + wv * 16 * 256;
+        if (end - 1 - g >= 15) {
+            load_rows16(kb, ko, to, lds, lane);
+            load_rows16(vb, vo, to + kSide, lds, lane);
+        } else {  // the group holds the last token
+            load_rows16(kb, row_offsets<true>(lane, end - 1 - g), to, lds, lane);
+            load_rows16(vb, row_offsets<false>(lane, end - 1 - g), to + kSide, lds, lane);
+        }
+    };
+    if (t0 < t1) issue(t0, 0);
+    for (int tile = t0; tile < t1; ++tile) {
+        const int buf = (tile - t0) & 1;
+        dma_wait<0>();
+        lds_reads_done();
+        barrier_only();
+        if (tile + 1 < t1) issue(tile + 1, buf ^ 1);
+        if (w0 >= rows || tile * kTile > past + last_t) continue;
+        const char* keys = lds + buf * kBuf;
+        f32x16 s[2];
+        tile_logits<DT, 2>(keys, lane, qf, s);
+        uint32_t mapped = 15u;
+        if constexpr (PAGED)
+            mapped = uniform(s_mapped[buf][0] | s_mapped[buf][1] << 1 | s_mapped[buf][2] << 2 | s_mapped[buf][3] << 3);
+        if (tile * kTile + kTile - 1 > past + first_t || mapped != 15u)
+            mask_logits<2>(s, lane, past + t - tile * kTile, mapped);
+        tile_update<DT, 2, ODT == kF32>(st, s, keys + kSide, lane, a.scale_log2e);
+    }
+    float lo, hi;
+    both_halves(st.l, lo, hi);
+    const float l = lo + hi;
+    if (w0 + (lane & 31) >= rows) return;
+    if (a.parts == 1) {
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                store4<ODT>(a.out, qrow * kD + 32 * c + 2 * i + 4 * (lane >> 5), st.o[c][i] * inv, st.o[c][i + 1] * inv,
+                            st.o[c][i + 2] * inv, st.o[c][i + 3] * inv);
+        if (a.lse && lane < 32) a.lse[qrow] = log_sum(st.m, l);
+        return;
+    }
+    const int64_t pr = ((static_cast<int64_t>(pl.unit) * a.tiles + pl.tile) * a.parts + pl.part) * kRowsTile + 32 * wv + (lane & 31);
+    if (lane < 32) reinterpret_cast<float2*>(a.part_ml)[pr] = make_float2(st.m, l);
+    if (t0 < t1) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                store4<kF32>(a.part_o, pr * kD + 32 * c + 2 * i + 4 * (lane >> 5), st.o[c][i], st.o[c][i + 1], st.o[c][i + 2],
+                             st.o[c][i + 3]);
+    }
+}
+
+template <int DT, int ODT, bool PAGED>
+__global__ __launch_bounds__(kBlock, 2) void chunk_tokens_kernel(const ChunkAttn a) {
+    constexpr int kTile = 32, kSide = kTile * 256;
+    __shared__ struct {
+        __align__(16) char tiles[4 * 2 * kSide];  // per wavefront keys, values; at the end the wavefronts' outputs
+        float m[4][32], l[4][32];
+    } shared;
+    char* lds = shared.tiles;
+    auto &s_m = shared.m, &s_l = shared.l;
+    const int lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
+    const Place pl = place_of(blockIdx.x, a.B * a.cv.Hkv, a.tiles, a.parts);
+    const int b = pl.unit / a.cv.Hkv, h = pl.unit % a.cv.Hkv;
+    const int past = chunk_past(a.ch, b, a.cv.Lmax), nn = chunk_new(a.ch, b, past, a.cv.Lmax);
+    const int rows = nn * a.R;
+    if (rows == 0) return;
+    const int end = past + nn, n_tiles = (end + kTile - 1) / kTile;
+    const int steps = (n_tiles + 3) / 4;
+    const int s0 = static_cast<int>(static_cast<int64_t>(steps) * pl.part / a.parts);
+    const int s1 = static_cast<int>(static_cast<int64_t>(steps) * (pl.part + 1) / a.parts);
+
+    const int mine = min(lane & 31, rows - 1), t = mine / a.R;
+    const int64_t qrow = (static_cast<int64_t>(b) * a.ch.n + t) * a.Hq + h * a.R + mine % a.R;
+    u32x4 qf[8];
+    load_queries<DT>(a.q + qrow * kD, lane, qf);
+    RowState st;
+    init_rows(st);
+
+    char* keys = lds + wv * 2 * kSide;
+    char* values = keys + kSide;
+    const RowOffsets ko = row_offsets<true>(lane, 15), vo = row_offsets<false>(lane, 15);
+    uint32_t mapped = 3u;
+    // the two 16-token groups of one of this wavefront's tiles, keys and values one after the other
+    auto issue = [&](const uint16_t* x, int tile, bool is_key) {
+        uint32_t got = 0;
+#pragma unroll
+        for (int g2 = 0; g2 < 2; ++g2) {
+            int g = tile * kTile + 16 * g2;
+            if (g >= end) g = (end - 1) & ~15;
+            const uint16_t* base = group_row(x, cache_row(a.cv, b, h, g));
+            got |= (base != nullptr) << g2;
+            const int last = min(end - 1 - g, 15);
+            RowOffsets r = is_key ? ko : vo;
+            if (last < 15) r = is_key ? row_offsets<true>(lane, last) : row_offsets<false>(lane, last);
+            load_rows16(base, r, (is_key ? keys : values) - lds + g2 * 16 * 256, lds, lane);
+        }
+        return got;
+    };
+    int tile = 4 * s0 + wv;
+    const int stop = min(4 * s1, n_tiles);
+    uint32_t next = 3u;
+    if (tile < stop) {
+        mapped = issue(a.K, tile, true);
+        issue(a.V, tile, false);
+    }
+    for (; tile < stop; tile += 4) {
+        const bool more = tile + 4 < stop;
+        dma_wait<8>();
+        if constexpr (PAGED) {
+            if (mapped != 3u) dma_wait<0>();  // fewer loads than counted
+        }
+        f32x16 s[1];
+        tile_logits<DT, 1>(keys, lane, qf, s);
+        lds_reads_done();
+        if (more) next = issue(a.K, tile + 4, true);
+        if (tile * kTile + kTile - 1 > past || mapped != 3u) mask_logits<1>(s, lane, past + t - tile * kTile, mapped);
+        if (more && (!PAGED || next == 3u))
+            dma_wait<8>();
+        else
+            dma_wait<0>();
+        tile_update<DT, 1, ODT == kF32>(st, s, values, lane, a.scale_log2e);
+        lds_reads_done();
+        if (more) issue(a.V, tile + 4, false);
+        mapped = next;
+    }
+    float lo, hi;
+    both_halves(st.l, lo, hi);
+    st.l = lo + hi;
+    __syncthreads();
+    // the four wavefronts' states of each row, joined
+    float* so = reinterpret_cast<float*>(lds) + wv * 32 * kD;
+    if (lane < 32) {
+        s_m[wv][lane] = st.m;
+        s_l[wv][lane] = st.l;
+    }
+    if ((lane & 31) < rows) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<float4*>(so + (lane & 31) * kD + 32 * c + 2 * i + 4 * (lane >> 5)) =
+                    make_float4(st.o[c][i], st.o[c][i + 1], st.o[c][i + 2], st.o[c][i + 3]);
+    }
+    __syncthreads();
+    const int n_rows = min(rows, 32);
+    for (int e = threadIdx.x; e < n_rows * (kD / 4); e += kBlock) {
+        const int r = e / (kD / 4), d = (e % (kD / 4)) * 4;
+        float M = kNegBig, l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) M = fmaxf(M, s_m[w][r]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = fast_exp2(s_m[w][r] - M);
+            const float4 x = *reinterpret_cast<const float4*>(reinterpret_cast<float*>(lds) + (w * 32 + r) * kD + d);
+            l += s_l[w][r] * f;
+            o[0] += x.x * f, o[1] += x.y * f, o[2] += x.z * f, o[3] += x.w * f;
+        }
+        if (a.parts == 1) {
+            const int64_t at = (static_cast<int64_t>(b) * a.ch.n + r / a.R) * a.Hq + h * a.R + r % a.R;
+            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+            store4<ODT>(a.out, at * kD + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+            if (a.lse && d == 0) a.lse[at] = log_sum(M, l);
+        } else {
+            const int64_t pr = (static_cast<int64_t>(pl.unit) * a.parts + pl.part) * kTokensTile + r;
+            store4<kF32>(a.part_o, pr * kD + d, o[0], o[1], o[2], o[3]);
+            if (d == 0) reinterpret_cast<float2*>(a.part_ml)[pr] = make_float2(M, l);
+        }
+    }
+}
+
+// The states of one row's parts, joined in their order: 32 lanes of four channels, eight parts at a time.
+template <int ODT>
+__global__ __launch_bounds__(kBlock) void chunk_join_kernel(const ChunkAttn a, int tile_rows) {
+    __shared__ float s_sum[8];
+    __shared__ float4 s_o[8][32];
+    const int64_t row = blockIdx.x;  // of [unit][n * R]
+    const int per = a.ch.n * a.R, u = static_cast<int>(row / per), m = static_cast<int>(row % per);
+    const int b = u / a.cv.Hkv, h = u % a.cv.Hkv;
+    const int past = chunk_past(a.ch, b, a.cv.Lmax), nn = chunk_new(a.ch, b, past, a.cv.Lmax);
+    if (m >= nn * a.R) return;
+    const int64_t p0 = (static_cast<int64_t>(u) * a.tiles + m / tile_rows) * a.parts;
+    const int tid = threadIdx.x, g = tid >> 5, c4 = tid & 31;
+    // (every wavefront of the workgroup reads all the maxima: no exchange needed for the largest)
+    float M = kNegBig;
+    float2 ml = make_float2(kNegBig, 0.0f);
+    for (int p = 0; p < a.parts; ++p)
+        M = fmaxf(M, reinterpret_cast<const float2*>(a.part_ml)[(p0 + p) * tile_rows + m % tile_rows].x);
+    float l = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int p = g; p < a.parts; p += 8) {
+        const int64_t at = (p0 + p) * tile_rows + m % tile_rows;
+        ml = reinterpret_cast<const float2*>(a.part_ml)[at];
+        if (ml.y <= 0.0f) continue;  // a part without tokens has not written its rows
+        const float f = fast_exp2(ml.x - M);
+        const float4 x = reinterpret_cast<const float4*>(a.part_o)[at * (kD / 4) + c4];
+        l += ml.y * f;
+        o.x += x.x * f, o.y += x.y * f, o.z += x.z * f, o.w += x.w * f;
+    }
+    s_o[g][c4] = o;
+    if (c4 == 0) s_sum[g] = l;
+    __syncthreads();
+    if (g != 0) return;
+    l = s_sum[0];
+#pragma unroll
+    for (int x = 1; x < 8; ++x) {
+        l += s_sum[x];
+        const float4 y = s_o[x][c4];
+        o.x += y.x, o.y += y.y, o.z += y.z, o.w += y.w;
+    }
+    const int64_t at = (static_cast<int64_t>(b) * a.ch.n + m / a.R) * a.Hq + h * a.R + m % a.R;
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    store4<ODT>(a.out, at * kD + 4 * c4, o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    if (a.lse && c4 == 0) a.lse[at] = log_sum(M, l);
+}
+
+// Form and split of a call.  The `rows` form runs two workgroups to a compute unit, as does the `tokens` form.
+struct ChunkPlan {
+    bool tokens;
+    int tiles, parts, tile_rows;
+};
+static ChunkPlan chunk_plan(const Dims& d, int n) {
+    ChunkPlan p;
+    const int64_t rows = static_cast<int64_t>(n) * d.R;
+    p.tokens = rows <= kTokensTile;
+    p.tile_rows = p.tokens ? kTokensTile : kRowsTile;
+    p.tiles = static_cast<int>((rows + p.tile_rows - 1) / p.tile_rows);
+    const int64_t groups = static_cast<int64_t>(d.units()) * p.tiles;
+    int64_t parts = (512 + groups - 1) / groups;
+    const int64_t most = (d.Lmax + 511) / 512;  // at least 512 tokens to a part
+    if (parts > most) parts = most;
+    if (parts > kMaxParts) parts = kMaxParts;
+    p.parts = static_cast<int>(parts < 1 ? 1 : parts);
+    return p;
+}
+
+static size_t plan_rows(const Dims& d, const ChunkPlan& p) {
+    return p.parts == 1 ? 0 : static_cast<size_t>(d.units()) * p.tiles * p.parts * p.tile_rows;
+}
+
+size_t chunk_attn_bytes(const Dims& d, int n) {
+    // the most that any chunk of up to n tokens needs: fewer row tiles have more parts
+    size_t most = 0;
+    for (int64_t m = 1; m <= n; m = m < 1024 ? m + 1 : m * 2) {
+        const size_t r = plan_rows(d, chunk_plan(d, static_cast<int>(m)));
+        if (r > most) most = r;
+    }
+    const size_t r = plan_rows(d, chunk_plan(d, n));
+    return (r > most ? r : most) * (kD + 2) * 4;
+}
 
 hipError_t launch_chunk_attn(const Dims& d, const CacheView& c, const ChunkView& ch, const void* q, const void* K,
-                             const void* V, float scale, void* out, float* lse, void*, hipStream_t s) {
-    const int nblk = (d.R + kSharedHeads - 1) / kSharedHeads;
-    const int64_t grid = static_cast<int64_t>(d.B) * ch.n * d.Hkv * nblk;
-    if (grid > 0x7fffffff / kBlock) return hipErrorInvalidConfiguration;
+                             const void* V, float scale, void* out, float* lse, void* ws, hipStream_t s) {
+    const ChunkPlan p = chunk_plan(d, ch.n);
+    const int64_t grid = static_cast<int64_t>(d.units()) * p.tiles * p.parts, join = static_cast<int64_t>(d.rows()) * ch.n;
+    if (grid > 0x7fffffff / kBlock || (p.parts > 1 && join > 0x7fffffff / kBlock)) return hipErrorInvalidConfiguration;
     const float sl2 = (scale > 0.0f ? scale : 1.0f / sqrtf(static_cast<float>(kD))) * 1.4426950408889634f;
-#define SIK_CHUNK(DTV, ODTV)                                                                                       \
-    launch_kernel(chunk_attn_kernel<DTV, ODTV>, static_cast<int>(grid), kBlock, s, static_cast<const uint16_t*>(q), \
-                  static_cast<const uint16_t*>(K), static_cast<const uint16_t*>(V), c, ch, d.Hq, d.R, nblk, sl2, out, lse)
-    if (d.kv_dtype == kBF16) return d.out_dtype == kF32 ? SIK_CHUNK(kBF16, kF32) : SIK_CHUNK(kBF16, kBF16);
-    return d.out_dtype == kF32 ? SIK_CHUNK(kF16, kF32) : SIK_CHUNK(kF16, kF16);
+    float* po = static_cast<float*>(ws);
+    const ChunkAttn a{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(K), static_cast<const uint16_t*>(V),
+                      c, ch, d.B, d.Hq, d.R, p.tiles, p.parts, sl2, out, lse, po, po + plan_rows(d, p) * kD};
+    hipError_t e = hipErrorInvalidValue;
+#define SIK_CHUNK(DTV, ODTV)                                                                                                \
+    e = p.tokens ? (c.table ? launch_kernel(chunk_tokens_kernel<DTV, ODTV, true>, static_cast<int>(grid), kBlock, s, a)     \
+                            : launch_kernel(chunk_tokens_kernel<DTV, ODTV, false>, static_cast<int>(grid), kBlock, s, a))   \
+                 : (c.table ? launch_kernel(chunk_rows_kernel<DTV, ODTV, true>, static_cast<int>(grid), kBlock, s, a)       \
+                            : launch_kernel(chunk_rows_kernel<DTV, ODTV, false>, static_cast<int>(grid), kBlock, s, a));    \
+    if (e == hipSuccess && p.parts > 1)                                                                                     \
+        e = launch_kernel(chunk_join_kernel<ODTV>, static_cast<int>(join), kBlock, s, a, p.tile_rows)
+    if (d.kv_dtype == kBF16) {
+        if (d.out_dtype == kF32) {
+            SIK_CHUNK(kBF16, kF32);
+        } else {
+            SIK_CHUNK(kBF16, kBF16);
+        }
+    } else if (d.out_dtype == kF32) {
+        SIK_CHUNK(kF16, kF32);
+    } else {
+        SIK_CHUNK(kF16, kF16);
+    }
 #undef SIK_CHUNK
+    return e;
 }
 
 }  // namespace sik
