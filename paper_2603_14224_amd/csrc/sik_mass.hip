@@ -1,50 +1,135 @@
 // Attention weight that each cached token receives from the last queries of a chunk.
-#include "sik_chunk.h"
+//
+// A wavefront owns 32 tokens: their keys stay in its registers as the second operand, the queries pass by as the first, 32
+// rows at a time through LDS (loaded one tile ahead, shared by the four wavefronts of a workgroup).  A lane then has one token
+// (column l % 32) and half of the tile's queries in its registers, so the weights are summed in the lane: no exchange, no
+// atomics, one order of additions.  Rows as in chunk attention: token t of the chunk and head r of the group are row t R + r.
+#include "sik_mma.h"
 
 namespace sik {
 
-// 16 lanes own one token: its key stays in registers while the queries pass, nothing is shared and no sum depends on an order
-// of arrival.
+constexpr int kMassRows = 32;
+
+struct MassArgs {
+    const uint16_t *q, *K;
+    const float* lse;
+    CacheView cv;
+    ChunkView ch;
+    int Hq, R, blocks, n_obs;
+    float scale_log2e;
+    const float* before;
+    float* mass;
+};
+
 template <int DT>
-__global__ __launch_bounds__(kBlock) void mass_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ K,
-                                                      const float* __restrict__ lse, CacheView cv, ChunkView ch, int Hq,
-                                                      int R, int nblk, int n_obs, float scale_log2e,
-                                                      const float* before, float* mass) {
-    const int lane = threadIdx.x & 63, p = lane & 15;
-    const int blk = blockIdx.x % nblk, u = blockIdx.x / nblk, h = u % cv.Hkv, b = u / cv.Hkv;
-    const int j = blk * (kBlock / 16) + (threadIdx.x >> 4);
-    const int past = chunk_past(ch, b, cv.Lmax), nn = chunk_new(ch, b, past, cv.Lmax);
-    if (j >= past + nn) return;
-    const int64_t row = cache_row(cv, b, h, j);
-    const uint4 k = row < 0 ? make_uint4(0u, 0u, 0u, 0u) : reinterpret_cast<const uint4*>(K + row * kD)[p];
-    float sum = 0.0f;
-    for (int t = max(max(0, nn - n_obs), j - past); t < nn && row >= 0; ++t) {
-        for (int r = 0; r < R; ++r) {
-            const int64_t qr = (static_cast<int64_t>(b) * ch.n + t) * Hq + h * R + r;
-            const uint4 x = reinterpret_cast<const uint4*>(q + qr * kD)[p];
-            float dot = dot2_acc<DT>(x.x, k.x, 0.0f);
-            dot = dot2_acc<DT>(x.y, k.y, dot);
-            dot = dot2_acc<DT>(x.z, k.z, dot);
-            dot = dot2_acc<DT>(x.w, k.w, dot);
-            const float l = lse[qr];
-            if (l > -1e30f) sum += fast_exp2(fmaf(row16_sum(dot), scale_log2e, -l * 1.4426950408889634f));
+__global__ __launch_bounds__(kBlock, 4) void mass_kernel(const MassArgs a) {
+    __shared__ struct {
+        __align__(16) char q[2][kMassRows * 256];
+        __align__(16) float lse[2][kMassRows];  // in powers of two; +infinity: the row contributes nothing
+        __align__(16) int last[2][kMassRows];   // last token that the row attends
+    } lds;
+    const int lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
+    const int u = blockIdx.x / a.blocks, b = u / a.cv.Hkv, h = u % a.cv.Hkv;
+    const int key0 = (blockIdx.x % a.blocks) * (4 * 32);
+    const int past = chunk_past(a.ch, b, a.cv.Lmax), nn = chunk_new(a.ch, b, past, a.cv.Lmax);
+    const int end = past + nn;
+    if (key0 >= end) return;
+
+    const int key = key0 + 32 * wv + (lane & 31);
+    const int64_t krow = cache_row(a.cv, b, h, min(key, end - 1));
+    u32x4 kf[8];
+#pragma unroll
+    for (int step = 0; step < 8; ++step)
+        kf[step] = krow < 0 ? u32x4{0u, 0u, 0u, 0u}
+                            : *reinterpret_cast<const u32x4*>(a.K + krow * kD + 16 * step + 8 * (lane >> 5));
+
+    // rows of the queries that count and attend a token of this workgroup
+    const int t_begin = max(max(nn - a.n_obs, 0), key0 - past);
+    const int m0 = t_begin * a.R, rows = nn * a.R;
+    const int tiles = t_begin < nn ? (rows - m0 + kMassRows - 1) / kMassRows : 0;
+    const int64_t chunk_row = static_cast<int64_t>(b) * a.ch.n;
+    // this lane's two rows of the loads (8 wv + 4 i + lane / 16 of a tile) and the first wavefront's row of the sums
+    auto load = [&](int tile, int buf, float& l, int& last) {
+        const int first = m0 + tile * kMassRows, t_first = first / a.R;
+        const uint16_t* base = uniform(a.q + ((chunk_row + t_first) * a.Hq + h * a.R) * kD);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = 8 * wv + 4 * i + (lane >> 4), m = min(first + r, rows - 1), t = m / a.R;
+            const uint32_t off = (static_cast<uint32_t>(t - t_first) * a.Hq + (m - t * a.R)) * 256u +
+                                 (((lane & 15) ^ key_swizzle(r)) << 4);
+            dma_16(base, off, uniform(static_cast<int>(lds_offset(lds.q[buf]) + (8 * wv + 4 * i) * 256)));
         }
+        if (wv == 0 && lane < kMassRows) {
+            const int m = first + lane, t = m / a.R;
+            l = __builtin_inff();
+            last = past + t;
+            if (m < rows) {
+                const float x = a.lse[(chunk_row + t) * a.Hq + h * a.R + (m - t * a.R)];
+                if (x > -__builtin_inff()) l = x * 1.4426950408889634f;
+            }
+        }
+    };
+    auto publish = [&](int buf, float l, int last) {
+        if (wv == 0 && lane < kMassRows) {
+            lds.lse[buf][lane] = l;
+            lds.last[buf][lane] = last;
+        }
+    };
+    float l = 0.0f, sum = 0.0f;
+    int last = 0;
+    if (tiles > 0) {
+        load(0, 0, l, last);
+        publish(0, l, last);
     }
-    const int64_t at = static_cast<int64_t>(u) * cv.Lmax + j;
-    if (p == 0) mass[at] = (before ? before[at] : 0.0f) + sum;
+    for (int tile = 0; tile < tiles; ++tile) {
+        const int buf = tile & 1;
+        dma_wait<0>();
+        lds_reads_done();
+        barrier_only();
+        const bool more = tile + 1 < tiles;
+        if (more) load(tile + 1, buf ^ 1, l, last);
+        f32x16 s{};
+#pragma unroll
+        for (int step = 0; step < 8; ++step) s = mma32<DT>(row_fragment(lds.q[buf], lane, step), kf[step], s);
+        if (key0 + 32 * wv + 31 > past + (m0 + tile * kMassRows) / a.R) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int4 x = *reinterpret_cast<const int4*>(&lds.last[buf][8 * g + 4 * (lane >> 5)]);
+                s[4 * g] = key > x.x ? -__builtin_inff() : s[4 * g];
+                s[4 * g + 1] = key > x.y ? -__builtin_inff() : s[4 * g + 1];
+                s[4 * g + 2] = key > x.z ? -__builtin_inff() : s[4 * g + 2];
+                s[4 * g + 3] = key > x.w ? -__builtin_inff() : s[4 * g + 3];
+            }
+        }
+        float part = 0.0f;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float4 x = *reinterpret_cast<const float4*>(&lds.lse[buf][8 * g + 4 * (lane >> 5)]);
+            part += (fast_exp2(fmaf(s[4 * g], a.scale_log2e, -x.x)) + fast_exp2(fmaf(s[4 * g + 1], a.scale_log2e, -x.y))) +
+                    (fast_exp2(fmaf(s[4 * g + 2], a.scale_log2e, -x.z)) + fast_exp2(fmaf(s[4 * g + 3], a.scale_log2e, -x.w)));
+        }
+        sum += part;
+        if (more) publish(buf ^ 1, l, last);
+    }
+    float lo, hi;
+    both_halves(sum, lo, hi);
+    sum = krow < 0 ? 0.0f : lo + hi;
+    if (lane < 32 && key < end) {
+        const int64_t at = static_cast<int64_t>(u) * a.cv.Lmax + key;
+        a.mass[at] = (a.before ? a.before[at] : 0.0f) + sum;
+    }
 }
 
 hipError_t launch_mass(const Dims& d, const CacheView& c, const ChunkView& ch, const void* q, const void* K, float scale,
                        const float* lse, int n_obs, const float* before, float* mass, hipStream_t s) {
-    const int nblk = (d.Lmax + kBlock / 16 - 1) / (kBlock / 16);
-    const int64_t grid = static_cast<int64_t>(nblk) * d.units();
+    const int blocks = (d.Lmax + 127) / 128;
+    const int64_t grid = static_cast<int64_t>(blocks) * d.units();
     if (grid > 0x7fffffff / kBlock) return hipErrorInvalidConfiguration;
     const float sl2 = (scale > 0.0f ? scale : 1.0f / sqrtf(static_cast<float>(kD))) * 1.4426950408889634f;
-#define SIK_MASS(DTV)                                                                                                \
-    launch_kernel(mass_kernel<DTV>, static_cast<int>(grid), kBlock, s, static_cast<const uint16_t*>(q),              \
-                  static_cast<const uint16_t*>(K), lse, c, ch, d.Hq, d.R, nblk, n_obs, sl2, before, mass)
-    return d.kv_dtype == kBF16 ? SIK_MASS(kBF16) : SIK_MASS(kF16);
-#undef SIK_MASS
+    const MassArgs a{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(K), lse, c, ch, d.Hq, d.R, blocks, n_obs,
+                     sl2, before, mass};
+    return d.kv_dtype == kBF16 ? launch_kernel(mass_kernel<kBF16>, static_cast<int>(grid), kBlock, s, a)
+                               : launch_kernel(mass_kernel<kF16>, static_cast<int>(grid), kBlock, s, a);
 }
 
 }  // namespace sik
