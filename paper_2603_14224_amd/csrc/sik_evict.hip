@@ -1,104 +1,478 @@
 // Eviction by accumulated attention weight: the tokens that stay, in ascending order, and the cache cut down to them.
+//
+// The cut is found by a radix selection on order-preserving keys of 32 bits, in digits of 11, 11 and 10 bits; what stays is
+// placed from bit counts, in token order, so the list needs no sort and no atomics decide an order.  Short caches: one
+// workgroup per (sequence, KV head) holds the weights in its registers.  Longer ones in three launches of many workgroups, a
+// chunk of tokens each: `count` (first digit of every chunk), `collect` (every workgroup adds the chunks' counts up, finds the
+// cut's bin and writes its tokens of that bin, a few per cent, behind those of the chunks before), `place` (the other two
+// digits from those tokens alone, then the chunk's part of the list).
 #include "sik_chunk.h"
 
 namespace sik {
 
 constexpr int kEvictBlock = 1024;
+constexpr int kDigitBins = 2048;   // of the first two digits; the last one has 1024
+constexpr int kChunkTokens = 8192; // tokens of a chunk, more where there would be more than kEvictChunks of them
+constexpr int kEvictChunks = 64;
+constexpr int kEvictDirect = 8192; // caches up to this length take one workgroup per row (8 weights per thread)
 
-// One workgroup per (sequence, KV head): the threshold key by four passes of 8-bit digits over the weights between the kept
-// ends, then one pass in token order that places what is above it and the first ones that equal it.
-__global__ __launch_bounds__(kEvictBlock) void evict_select_kernel(EvictArgs a, int Hkv, int Lmax) {
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t s_digit, s_need;
-    __shared__ uint32_t wsum[2][kEvictBlock / kWave];
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));  // rows start at any multiple of 4 bytes
+
+struct EvictRow {
+    int L, lo, hi, need;  // tokens; those between the kept ends; how many of them stay
+    __device__ __forceinline__ bool inner(int i) const { return i >= lo && i < hi; }
+};
+__device__ __forceinline__ EvictRow evict_row(const EvictArgs& a, int b, int Lmax) {
+    EvictRow r;
+    r.L = min(max(a.seq_len[b], 0), Lmax);
+    r.lo = a.n_sink;
+    r.hi = r.L - a.n_recent;
+    r.need = a.n_keep - a.n_sink - a.n_recent;
+    return r;
+}
+
+// Counts of `bin` over the lanes that are `on`.  Equal weights (vanished ones above all) would meet in one counter: the lanes
+// that share the first lane's bin are counted by one addition.
+__device__ __forceinline__ void count_bins(uint32_t* hist, uint32_t bin, bool on) {
+    const uint64_t some = __ballot(on);
+    if (some == 0) return;
+    const int first = __ffsll(static_cast<unsigned long long>(some)) - 1;
+    const uint32_t lead = __builtin_amdgcn_readlane(bin, first);
+    const bool same = on && bin == lead;
+    const uint64_t m = __ballot(same);
+    if (on && !same) atomicAdd(&hist[bin], 1u);
+    if (static_cast<int>(threadIdx.x & 63) == first) atomicAdd(&hist[lead], static_cast<uint32_t>(__popcll(m)));
+}
+
+__device__ __forceinline__ f32x4_any load4(const float* m, int i, int L) {
+    if (i + 4 <= L) return *reinterpret_cast<const f32x4_any*>(m + i);
+    f32x4_any v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+        if (i + e < L) v[e] = m[i + e];
+    return v;
+}
+
+// The bin, from the top, in which the need-th token lies, and how many of that bin's tokens are still needed.  Thread t of
+// BLOCK holds the counts of bins NB (BLOCK - 1 - t) ..; exactly one thread finds the bin.
+template <int BLOCK, int NB>
+__device__ __forceinline__ void find_digit(const uint32_t (&c)[NB], uint32_t& digit, uint32_t& need, uint32_t* totals,
+                                           uint32_t* found) {
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    const int u = blockIdx.x, b = u / Hkv;
-    const int L = min(max(a.seq_len[b], 0), Lmax);
-    const float* m = a.mass + static_cast<int64_t>(u) * Lmax;
-    int32_t* keep = a.keep + static_cast<int64_t>(u) * a.n_keep;
-    if (a.new_len && u % Hkv == 0 && tid == 0) a.new_len[b] = min(L, a.n_keep);
-    if (L <= a.n_keep) {
-        for (int i = tid; i < a.n_keep; i += kEvictBlock) keep[i] = i < L ? i : -1;
-        return;
-    }
-    const int lo = a.n_sink, hi = L - a.n_recent;
-    uint32_t need = a.n_keep - a.n_sink - a.n_recent, prefix = 0;
-    for (int sh = 24; sh >= 0 && need > 0; sh -= 8) {
-        if (tid < 256) hist[tid] = 0;
-        __syncthreads();
-        for (int i = lo + tid; i < hi; i += kEvictBlock) {
-            const uint32_t key = float_to_key(m[i]);
-            if (sh == 24 || (key >> (sh + 8)) == prefix) atomicAdd(&hist[(key >> sh) & 255], 1u);
-        }
-        __syncthreads();
-        if (tid == 0) {
-            uint32_t n = need, dg = 255;
-            while (dg > 0 && hist[dg] < n) n -= hist[dg--];
-            s_digit = dg;
-            s_need = n;
-        }
-        __syncthreads();
-        prefix = prefix << 8 | s_digit;
-        need = s_need;
-    }
-    // prefix: the key at the cut (need > 0 of the tokens that equal it stay)
-    const bool any = a.n_keep > a.n_sink + a.n_recent;
-    uint32_t placed = 0, equal = 0;
-    for (int i0 = 0; i0 < L; i0 += kEvictBlock) {
-        const int i = i0 + tid;
-        const bool end = i < L && (i < lo || i >= hi);
-        const uint32_t key = i < L && !end && any ? float_to_key(m[i]) : 0u;
-        const bool mid = i < L && !end && any;
-        const bool eq = mid && key == prefix, sure = end || (mid && key > prefix);
-        const uint64_t me = __ballot(eq), ms = __ballot(sure), below = (1ull << lane) - 1;
-        if (lane == 0) {
-            wsum[0][wv] = __popcll(me);
-            wsum[1][wv] = __popcll(ms);
-        }
-        __syncthreads();
-        uint32_t e0 = equal, s0 = 0, et = 0, st = 0;
-        for (int w = 0; w < kEvictBlock / kWave; ++w) {
-            if (w < wv) {
-                e0 += wsum[0][w];
-                s0 += wsum[1][w];
+    uint32_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) mine += c[i];
+    const uint32_t incl = wave_inclusive_sum(mine);
+    if (lane == 63) totals[wv] = incl;
+    __syncthreads();
+    uint32_t before = incl - mine;
+    for (int w = 0; w < wv; ++w) before += totals[w];
+    if (before < need && need <= before + mine) {
+#pragma unroll
+        for (int i = NB - 1; i >= 0; --i) {
+            if (before < need && need <= before + c[i]) {
+                found[0] = NB * (BLOCK - 1 - tid) + i;
+                found[1] = need - before;
             }
-            et += wsum[0][w];
-            st += wsum[1][w];
+            before += c[i];
         }
-        const uint32_t e_rank = e0 + __popcll(me & below);
-        // kept before this token: the sure ones and as many of the equal ones as still fit
-        const uint32_t at = placed + s0 + __popcll(ms & below) + (min(e_rank, need) - min(equal, need));
-        if (sure || (eq && e_rank < need)) keep[at] = i;
-        placed += st + (min(equal + et, need) - min(equal, need));
-        equal += et;
-        __syncthreads();
+    }
+    __syncthreads();
+    digit = found[0];
+    need = found[1];
+}
+
+// Places what stays of four consecutive tokens per lane (from i): `sure` ones, and of those `equal` to the cut the first `need`.
+// ps, pe: sure and equal tokens before this wavefront's step, advanced by it.
+__device__ __forceinline__ void place4(int32_t* keep, int i, const bool (&sure)[4], const bool (&equal)[4], uint32_t need,
+                                       uint32_t& ps, uint32_t& pe) {
+    uint32_t cs = 0, ce = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        cs += sure[e];
+        ce += equal[e];
+    }
+    if (__ballot((cs | ce) != 0) == 0) return;
+    const uint32_t both = wave_inclusive_sum(cs | ce << 16);
+    uint32_t s = ps + (both & 0xffffu) - cs, q = pe + (both >> 16) - ce;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (sure[e] || (equal[e] && q < need)) keep[s + min(q, need)] = i + e;
+        s += sure[e];
+        q += equal[e];
+    }
+    const uint32_t all = __builtin_amdgcn_readlane(both, 63);
+    ps += all & 0xffffu;
+    pe += all >> 16;
+}
+
+// Sums of two counts over the wavefronts before this one; tot: [waves][2] of LDS.
+template <int WAVES>
+__device__ __forceinline__ void before_wave(uint32_t a, uint32_t b, uint32_t (*tot)[2], uint32_t& ba, uint32_t& bb) {
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    if (lane == 0) {
+        tot[wv][0] = a;
+        tot[wv][1] = b;
+    }
+    __syncthreads();
+    for (int w = 0; w < WAVES; ++w) {
+        if (w < wv) {
+            ba += tot[w][0];
+            bb += tot[w][1];
+        }
     }
 }
 
-// 16 lanes copy one kept row of K and of V.
+// ---- short caches: one workgroup per row ------------------------------------------------------------------------------
+__global__ __launch_bounds__(kEvictBlock) void evict_select_kernel(EvictArgs a, int Hkv, int Lmax) {
+    constexpr int kWaves = kEvictBlock / kWave, NV = kEvictDirect / (4 * kEvictBlock);
+    __shared__ uint32_t hist[kDigitBins];
+    __shared__ uint32_t totals[kWaves], found[2], s_tot[kWaves][2];
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int u = blockIdx.x, b = u / Hkv;
+    const EvictRow r = evict_row(a, b, Lmax);
+    const float* m = a.mass + static_cast<int64_t>(u) * Lmax;
+    int32_t* keep = a.keep + static_cast<int64_t>(u) * a.n_keep;
+    if (a.new_len && u % Hkv == 0 && tid == 0) a.new_len[b] = min(r.L, a.n_keep);
+    if (r.L <= a.n_keep) {
+        for (int i = tid; i < a.n_keep; i += kEvictBlock) keep[i] = i < r.L ? i : -1;
+        return;
+    }
+    f32x4_any v[NV];  // a wavefront's consecutive tokens, 256 a step
+    const int at = wv * (256 * NV) + 4 * lane;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = load4(m, at + 256 * i, r.L);
+    uint32_t cut = 0, need = r.need;
+    for (int digit = 0; digit < 3 && r.need > 0; ++digit) {
+        const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, above = digit == 1 ? 21 : 10;
+        hist[tid] = 0;
+        hist[tid + kEvictBlock] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t key = float_to_key(v[i][e]);
+                count_bins(hist, (key >> shift) & (digit == 2 ? 1023u : 2047u),
+                           r.inner(at + 256 * i + e) && (digit == 0 || (key >> above) == cut));
+            }
+        __syncthreads();
+        const uint32_t c[2] = {hist[2 * (kEvictBlock - 1 - tid)], hist[2 * (kEvictBlock - 1 - tid) + 1]};
+        uint32_t d;
+        find_digit<kEvictBlock>(c, d, need, totals, found);
+        cut = cut << (digit == 2 ? 10 : 11) | d;
+    }
+    bool sure[NV][4], equal[NV][4];
+    uint32_t ns = 0, ne = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int j = at + 256 * i + e;
+            const uint32_t key = float_to_key(v[i][e]);
+            sure[i][e] = j < r.L && (!r.inner(j) || (r.need > 0 && key > cut));
+            equal[i][e] = r.need > 0 && r.inner(j) && key == cut;
+            ns += __popcll(__ballot(sure[i][e]));
+            ne += __popcll(__ballot(equal[i][e]));
+        }
+    uint32_t ps = 0, pe = 0;
+    before_wave<kWaves>(ns, ne, s_tot, ps, pe);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) place4(keep, at + 256 * i, sure[i], equal[i], need, ps, pe);
+}
+
+// ---- long caches: a workgroup per chunk of `per` tokens -----------------------------------------------------------------
+struct EvictScratch {
+    uint32_t* counts;  // [unit][chunk][kDigitBins]  first digits
+    uint32_t* list;    // [unit][list_len]           keys of the tokens in the cut's bin, in token order
+    uint32_t* heads;   // [unit][chunk][4]           of the chunk: its first entry of the list, tokens that surely stay before
+                       //                            it; of the row: length of the list, how many of it stay
+    uint32_t* bins;    // [unit]                     the cut's bin
+    int chunks, per;
+    int64_t list_len;
+};
+
+__global__ __launch_bounds__(kBlock) void evict_count_kernel(EvictArgs a, int Hkv, int Lmax, EvictScratch w) {
+    __shared__ uint32_t hist[kDigitBins];
+    const int u = blockIdx.x / w.chunks, c = blockIdx.x % w.chunks;
+    const EvictRow r = evict_row(a, u / Hkv, Lmax);
+    if (r.L <= a.n_keep || r.need == 0) return;
+    for (int i = threadIdx.x; i < kDigitBins; i += kBlock) hist[i] = 0;
+    __syncthreads();
+    const float* m = a.mass + static_cast<int64_t>(u) * Lmax;
+    const int end = min(r.L, (c + 1) * w.per);
+    for (int i0 = c * w.per; i0 < end; i0 += 4 * kBlock) {  // (the whole workgroup: the counting uses ballots)
+        const int i = i0 + 4 * static_cast<int>(threadIdx.x);
+        const f32x4_any v = load4(m, i, i < end ? r.L : 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) count_bins(hist, float_to_key(v[e]) >> 21, i + e < end && r.inner(i + e));
+    }
+    __syncthreads();
+    uint32_t* out = w.counts + static_cast<int64_t>(blockIdx.x) * kDigitBins;
+    for (int i = threadIdx.x; i < kDigitBins; i += kBlock) out[i] = hist[i];
+}
+
+// A wavefront's quarter of a chunk: [first, last), in steps of 256 tokens, four per lane.
+__device__ __forceinline__ void quarter(const EvictScratch& w, const EvictRow& r, int c, int& first, int& last) {
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = ((w.per / 4 + 255) / 256) * 256;
+    const int end = min(r.L, (c + 1) * w.per);
+    first = min(c * w.per + wv * q, end);
+    last = min(first + q, end);
+}
+
+__global__ __launch_bounds__(kBlock) void evict_collect_kernel(EvictArgs a, int Hkv, int Lmax, EvictScratch w) {
+    constexpr int kWaves = kBlock / kWave, NB = kDigitBins / kBlock;
+    __shared__ uint32_t totals[kWaves], found[2], s_before, s_list, s_len, s_tot[kWaves][2];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int u = blockIdx.x / w.chunks, c = blockIdx.x % w.chunks;
+    const EvictRow r = evict_row(a, u / Hkv, Lmax);
+    if (r.L <= a.n_keep || r.need == 0 || c * w.per >= r.L) return;
+    // counts of this thread's bins over all chunks and over those before this one
+    uint32_t all[NB], before[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) all[i] = before[i] = 0;
+    const uint32_t* cp = w.counts + static_cast<int64_t>(u) * w.chunks * kDigitBins + NB * (kBlock - 1 - tid);
+    const int used = (r.L + w.per - 1) / w.per;
+#pragma unroll 4
+    for (int k = 0; k < used; ++k) {
+        uint32_t x[NB];
+#pragma unroll
+        for (int i = 0; i < NB; i += 4) {
+            const uint4 y = *reinterpret_cast<const uint4*>(cp + static_cast<int64_t>(k) * kDigitBins + i);
+            x[i] = y.x, x[i + 1] = y.y, x[i + 2] = y.z, x[i + 3] = y.w;
+        }
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            all[i] += x[i];
+            before[i] += k < c ? x[i] : 0u;
+        }
+    }
+    if (tid == 0) s_before = 0;
+    uint32_t bin, need = r.need;
+    find_digit<kBlock>(all, bin, need, totals, found);
+    uint32_t above = 0;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+        const uint32_t mine = NB * (kBlock - 1 - tid) + i;
+        if (mine > bin) above += before[i];
+        if (mine == bin) {
+            s_list = before[i];
+            s_len = all[i];
+        }
+    }
+    above = wave_sum(above);
+    if (lane == 0 && above) atomicAdd(&s_before, above);
+    // the tokens of that bin, in order
+    int first, last;
+    quarter(w, r, c, first, last);
+    const float* m = a.mass + static_cast<int64_t>(u) * Lmax;
+    uint32_t n = 0;
+    for (int i0 = first; i0 < last; i0 += 256) {
+        const int i = i0 + 4 * lane;
+        const f32x4_any v = load4(m, i, i < last ? r.L : 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) n += __popcll(__ballot(i + e < last && r.inner(i + e) && float_to_key(v[e]) >> 21 == bin));
+    }
+    uint32_t at = 0, none = 0;
+    before_wave<kWaves>(n, 0u, s_tot, at, none);
+    at += s_list;
+    if (tid == 0) {
+        const int cs = c * w.per;  // kept ends in front of the chunk stay as well
+        uint32_t* hd = w.heads + static_cast<int64_t>(blockIdx.x) * 4;
+        hd[0] = s_list;
+        hd[1] = s_before + min(cs, r.lo) + max(0, cs - max(r.hi, r.lo));
+        hd[2] = s_len;
+        hd[3] = need;
+        if (c == 0) w.bins[u] = bin;
+    }
+    uint32_t* list = w.list + u * w.list_len;
+    for (int i0 = first; i0 < last; i0 += 256) {
+        const int i = i0 + 4 * lane;
+        const f32x4_any v = load4(m, i, i < last ? r.L : 0);
+        bool in[4];
+        uint32_t k = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            in[e] = i + e < last && r.inner(i + e) && float_to_key(v[e]) >> 21 == bin;
+            k += in[e];
+        }
+        const uint32_t incl = wave_inclusive_sum(k);
+        uint32_t p = at + incl - k;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (in[e]) list[p++] = float_to_key(v[e]);
+        at += __builtin_amdgcn_readlane(incl, 63);
+    }
+}
+
+__global__ __launch_bounds__(kBlock) void evict_place_kernel(EvictArgs a, int Hkv, int Lmax, EvictScratch w) {
+    constexpr int kWaves = kBlock / kWave, NB = kDigitBins / kBlock;
+    __shared__ uint32_t hist[kDigitBins];
+    __shared__ uint32_t totals[kWaves], found[2], s_sure, s_equal, s_tot[kWaves][2];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int u = blockIdx.x / w.chunks, c = blockIdx.x % w.chunks;
+    const EvictRow r = evict_row(a, u / Hkv, Lmax);
+    int32_t* keep = a.keep + static_cast<int64_t>(u) * a.n_keep;
+    if (a.new_len && u % Hkv == 0 && c == 0 && tid == 0) a.new_len[u / Hkv] = min(r.L, a.n_keep);
+    const int cs = c * w.per;
+    if (r.L <= a.n_keep) {
+        for (int i = cs + tid; i < min(a.n_keep, cs + w.per); i += kBlock) keep[i] = i < r.L ? i : -1;
+        return;
+    }
+    if (cs >= r.L) return;
+    uint32_t cut = 0, need = 0, sure0, equal0 = 0;
+    const bool any = r.need > 0;
+    if (any) {
+        const uint32_t* hd = w.heads + static_cast<int64_t>(blockIdx.x) * 4;
+        const uint32_t mine = hd[0], len = hd[2];
+        sure0 = hd[1];
+        need = hd[3];
+        cut = w.bins[u];
+        const uint32_t* list = w.list + u * w.list_len;
+        if (tid == 0) s_sure = s_equal = 0;
+        for (int digit = 1; digit < 3; ++digit) {
+            for (int i = tid; i < kDigitBins; i += kBlock) hist[i] = 0;
+            __syncthreads();
+            for (uint32_t p = 0; p < len; p += kBlock) {
+                const uint32_t key = p + tid < len ? list[p + tid] : 0u;
+                count_bins(hist, digit == 1 ? (key >> 10) & 2047u : key & 1023u,
+                           p + tid < len && (digit == 1 || key >> 10 == cut));
+            }
+            __syncthreads();
+            uint32_t x[NB], d;
+#pragma unroll
+            for (int i = 0; i < NB; ++i) x[i] = hist[NB * (kBlock - 1 - tid) + i];
+            find_digit<kBlock>(x, d, need, totals, found);
+            cut = cut << (digit == 1 ? 11 : 10) | d;
+        }
+        uint32_t ns = 0, ne = 0;  // of the list's tokens in front of the chunk
+        for (uint32_t p = tid; p < mine; p += kBlock) {
+            const uint32_t key = list[p];
+            ns += key > cut;
+            ne += key == cut;
+        }
+        ns = wave_sum(ns);
+        ne = wave_sum(ne);
+        if (lane == 0 && (ns | ne)) {
+            atomicAdd(&s_sure, ns);
+            atomicAdd(&s_equal, ne);
+        }
+        __syncthreads();
+        sure0 += s_sure;
+        equal0 = s_equal;
+    } else {
+        sure0 = min(cs, r.lo) + max(0, cs - max(r.hi, r.lo));
+    }
+    int first, last;
+    quarter(w, r, c, first, last);
+    const float* m = a.mass + static_cast<int64_t>(u) * Lmax;
+    auto classes = [&](int i, bool (&sure)[4], bool (&equal)[4]) {
+        const f32x4_any v = load4(m, i, i < last ? r.L : 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t key = float_to_key(v[e]);
+            sure[e] = i + e < last && (!r.inner(i + e) || (any && key > cut));
+            equal[e] = any && i + e < last && r.inner(i + e) && key == cut;
+        }
+    };
+    uint32_t ns = 0, ne = 0;
+    for (int i0 = first; i0 < last; i0 += 256) {
+        bool sure[4], equal[4];
+        classes(i0 + 4 * lane, sure, equal);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            ns += __popcll(__ballot(sure[e]));
+            ne += __popcll(__ballot(equal[e]));
+        }
+    }
+    uint32_t ps = sure0, pe = equal0;
+    before_wave<kWaves>(ns, ne, s_tot, ps, pe);
+    for (int i0 = first; i0 < last; i0 += 256) {
+        bool sure[4], equal[4];
+        classes(i0 + 4 * lane, sure, equal);
+        place4(keep, i0 + 4 * lane, sure, equal, need, ps, pe);
+    }
+}
+
+// 16 lanes copy a kept row of K and of V, kRowsEach of them, all requested before the first is stored.
+constexpr int kRowsEach = 2;
 __global__ __launch_bounds__(kBlock) void evict_rows_kernel(EvictArgs a, CacheView cv, int nblk) {
     const int p = threadIdx.x & 15;
     const int u = blockIdx.x / nblk, b = u / cv.Hkv, h = u % cv.Hkv;
-    const int i = (blockIdx.x % nblk) * (kBlock / 16) + (threadIdx.x >> 4);
-    if (i >= a.n_keep) return;
-    const int j = a.keep[static_cast<int64_t>(u) * a.n_keep + i];
-    if (j < 0) return;
-    const int64_t to = static_cast<int64_t>(u) * a.out_len + i;
-    if (a.mass_out && p == 0) a.mass_out[to] = a.mass[static_cast<int64_t>(u) * cv.Lmax + j];
-    if (!a.K_out) return;
-    const int64_t from = cache_row(cv, b, h, j);
-    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-    reinterpret_cast<uint4*>(a.K_out + to * kD)[p] = from < 0 ? zero : reinterpret_cast<const uint4*>(a.K + from * kD)[p];
-    reinterpret_cast<uint4*>(a.V_out + to * kD)[p] = from < 0 ? zero : reinterpret_cast<const uint4*>(a.V + from * kD)[p];
+    const int i0 = (blockIdx.x % nblk) * (kBlock / 16 * kRowsEach) + (threadIdx.x >> 4);
+    int j[kRowsEach];
+    int64_t from[kRowsEach];
+    uint4 k[kRowsEach], v[kRowsEach];
+#pragma unroll
+    for (int x = 0; x < kRowsEach; ++x) {
+        const int i = i0 + x * (kBlock / 16);
+        j[x] = i < a.n_keep ? a.keep[static_cast<int64_t>(u) * a.n_keep + i] : -1;
+    }
+#pragma unroll
+    for (int x = 0; x < kRowsEach; ++x) {
+        from[x] = j[x] < 0 || !a.K_out ? -1 : cache_row(cv, b, h, j[x]);
+        k[x] = v[x] = make_uint4(0u, 0u, 0u, 0u);
+        if (from[x] >= 0) {
+            k[x] = ld_stream(reinterpret_cast<const uint4*>(a.K + from[x] * kD) + p);
+            v[x] = ld_stream(reinterpret_cast<const uint4*>(a.V + from[x] * kD) + p);
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < kRowsEach; ++x) {
+        if (j[x] < 0) continue;
+        const int64_t to = static_cast<int64_t>(u) * a.out_len + i0 + x * (kBlock / 16);
+        if (a.mass_out && p == 0) a.mass_out[to] = a.mass[static_cast<int64_t>(u) * cv.Lmax + j[x]];
+        if (!a.K_out) continue;
+        reinterpret_cast<uint4*>(a.K_out + to * kD)[p] = k[x];
+        reinterpret_cast<uint4*>(a.V_out + to * kD)[p] = v[x];
+    }
 }
 
-size_t evict_bytes(const Dims&) { return 0; }
+static EvictScratch evict_plan(const Dims& d, void* ws, size_t* bytes) {
+    EvictScratch w{};
+    w.per = kChunkTokens;
+    const int least = (d.Lmax + kEvictChunks - 1) / kEvictChunks;
+    if (least > w.per) w.per = (least + 1023) / 1024 * 1024;
+    w.chunks = d.Lmax <= kEvictDirect ? 0 : (d.Lmax + w.per - 1) / w.per;
+    w.list_len = d.Lmax;
+    const int64_t units = d.units(), rows = units * w.chunks;
+    uint32_t* p = static_cast<uint32_t*>(ws);
+    w.counts = p;
+    w.heads = w.counts + rows * kDigitBins;
+    w.bins = w.heads + rows * 4;
+    w.list = w.bins + units;
+    *bytes = w.chunks ? static_cast<size_t>(rows * (kDigitBins + 4) + units + units * w.list_len) * 4 : 0;
+    return w;
+}
 
-hipError_t launch_evict(const Dims& d, const CacheView& c, const EvictArgs& a, void*, hipStream_t s) {
-    hipError_t e = launch_kernel(evict_select_kernel, d.units(), kEvictBlock, s, a, d.Hkv, d.Lmax);
-    if (e != hipSuccess || (!a.K_out && !a.mass_out)) return e;
-    const int nblk = (a.n_keep + kBlock / 16 - 1) / (kBlock / 16);
-    if (static_cast<int64_t>(nblk) * d.units() > 0x7fffffff / kBlock) return hipErrorInvalidConfiguration;
+size_t evict_bytes(const Dims& d) {
+    size_t n;
+    evict_plan(d, nullptr, &n);
+    return n;
+}
+
+hipError_t launch_evict(const Dims& d, const CacheView& c, const EvictArgs& a, void* ws, hipStream_t s) {
+    size_t bytes;
+    const EvictScratch w = evict_plan(d, ws, &bytes);
+    const int nblk = (a.n_keep + kBlock / 16 * kRowsEach - 1) / (kBlock / 16 * kRowsEach);
+    const bool rows = a.K_out || a.mass_out;
+    const int64_t chunks = static_cast<int64_t>(w.chunks) * d.units();
+    if (chunks > 0x7fffffff / kBlock || d.units() > 0x7fffffff / kEvictBlock ||
+        (rows && static_cast<int64_t>(nblk) * d.units() > 0x7fffffff / kBlock))
+        return hipErrorInvalidConfiguration;
+    hipError_t e;
+    if (w.chunks == 0) {
+        e = launch_kernel(evict_select_kernel, d.units(), kEvictBlock, s, a, d.Hkv, d.Lmax);
+    } else {
+        const int grid = static_cast<int>(chunks);
+        e = hipSuccess;
+        if (a.n_sink + a.n_recent < a.n_keep) {
+            e = launch_kernel(evict_count_kernel, grid, kBlock, s, a, d.Hkv, d.Lmax, w);
+            if (e == hipSuccess) e = launch_kernel(evict_collect_kernel, grid, kBlock, s, a, d.Hkv, d.Lmax, w);
+        }
+        if (e == hipSuccess) e = launch_kernel(evict_place_kernel, grid, kBlock, s, a, d.Hkv, d.Lmax, w);
+    }
+    if (e != hipSuccess || !rows) return e;
     return launch_kernel(evict_rows_kernel, nblk * d.units(), kBlock, s, a, c, nblk);
 }
 
