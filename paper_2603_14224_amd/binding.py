@@ -328,27 +328,38 @@ def sik_decode_step_profiled(layout, q, k_new, v_new, K, V, seq_len, mu, codeboo
 # ---- the prompt side of the cache.  These calls check types, shapes and devices of the tensors here; what the C ABI can
 # see (alignment, ranges, page sizes) it checks itself.
 
-def _tensor(name, t, dtype, shape=None, numel=None, optional=False):
+_has_gpu = None
+
+
+def _device():
+    """Index of the device that the calls run on (-1 without a GPU: the C side then validates and reports)."""
+    global _has_gpu
+    if _has_gpu is None:
+        _has_gpu = torch.cuda.is_available()
+    return torch.cuda.current_device() if _has_gpu else -1
+
+
+def _stream_of(dev):
+    return torch.cuda.current_stream(dev).cuda_stream if dev >= 0 else None
+
+
+def _tensor(name, t, dtype, dev, shape=None, numel=None, optional=False):
     """Address of a tensor after its checks, None for an absent optional one."""
     if t is None:
         if optional:
             return None
         raise ValueError(f"{name} is required")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name}: {t.dtype} given, {dtype} needed")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    if shape is not None and tuple(t.shape) != shape:
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)} given, {shape} needed")
     if numel is not None and t.numel() != numel:
         raise ValueError(f"{name}: {t.numel()} elements given, {numel} needed")
-    _on_device(name, t)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the call runs on device {dev}")
     return t.data_ptr()
-
-
-def _on_device(name, t):
-    if torch.cuda.is_available() and t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, the call runs on cuda:{torch.cuda.current_device()}")
 
 
 _SIK2TORCH = {SIK_F16: torch.float16, SIK_BF16: torch.bfloat16, SIK_F32: torch.float32}
@@ -358,73 +369,76 @@ def make_pages(page_table, page_len, n_pages) -> Pages:
     """Description of a paged cache: page_table [B, pages_per_seq] int32, pools of n_pages pages of page_len tokens."""
     if page_table.dim() != 2:
         raise ValueError("page_table must be [batch, pages per sequence]")
-    pages = Pages(_tensor("page_table", page_table, torch.int32), page_table.shape[1], int(page_len), int(n_pages))
+    pages = Pages(_tensor("page_table", page_table, torch.int32, _device()), page_table.shape[1], int(page_len), int(n_pages))
     pages.tensor = page_table
     return pages
 
 
 def make_chunk(n, seq_len, n_new=None, pages=None) -> Chunk:
     """A chunk of n new tokens per sequence (n_new[b] of them real) behind the seq_len[b] tokens in the cache."""
-    chunk = Chunk(int(n), _tensor("n_new", n_new, torch.int32, optional=True), _tensor("seq_len", seq_len, torch.int32),
-                  None if pages is None else ctypes.pointer(pages))
+    dev = _device()
+    chunk = Chunk(int(n), _tensor("n_new", n_new, torch.int32, dev, optional=True),
+                  _tensor("seq_len", seq_len, torch.int32, dev), None if pages is None else ctypes.pointer(pages))
     chunk.tensors = (seq_len, n_new, pages)
     return chunk
 
 
-def _check_chunk(layout, chunk):
+def _check_chunk(layout, chunk, dev):
     seq_len, n_new, pages = chunk.tensors
     if seq_len.numel() != layout.batch or (n_new is not None and n_new.numel() != layout.batch):
         raise ValueError("seq_len and n_new hold one length per sequence")
-    _check_page_table(layout, pages)
+    if seq_len.get_device() != dev:
+        raise ValueError(f"the chunk is on {seq_len.device}, the call runs on device {dev}")
+    _check_page_table(layout, pages, dev)
     return pages
 
 
-def _check_page_table(layout, pages):
-    if pages is not None and pages.tensor.shape[0] != layout.batch:
-        raise ValueError("page_table holds one row per sequence")
+def _check_page_table(layout, pages, dev):
+    if pages is not None and (pages.tensor.shape[0] != layout.batch or pages.tensor.get_device() != dev):
+        raise ValueError("page_table holds one row per sequence and lies on the device of the call")
 
 
-def _cache(name, t, layout, pages, optional=False):
-    """Address of one side of a contiguous or paged cache."""
+def _cache_shape(layout, pages):
+    """Shape of one side of a contiguous or paged cache."""
     if pages is None:
-        shape = (layout.batch, layout.n_kv_heads, layout.max_len, layout.head_dim)
-    else:
-        shape = (pages.n_pages, layout.n_kv_heads, pages.page_len, layout.head_dim)
-    return _tensor(name, t, _SIK2TORCH[layout.kv_dtype], shape, optional=optional)
+        return (layout.batch, layout.n_kv_heads, layout.max_len, layout.head_dim)
+    return (pages.n_pages, layout.n_kv_heads, pages.page_len, layout.head_dim)
 
 
-def _head_rows(name, t, layout, n, heads):
+def _head_rows(name, t, dtype, dev, shape):
     """Address and token stride of [B, n, heads, D] head rows, which may be part of a wider projection's output."""
-    if t.dtype != _SIK2TORCH[layout.kv_dtype] or tuple(t.shape) != (layout.batch, n, heads, layout.head_dim):
-        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} given, {_SIK2TORCH[layout.kv_dtype]} "
-                         f"{(layout.batch, n, heads, layout.head_dim)} needed")
-    D = layout.head_dim
-    stride = t.stride(1) if n > 1 else t.stride(0) if layout.batch > 1 else heads * D
-    if t.stride(3) != 1 or (heads > 1 and t.stride(2) != D) or (layout.batch > 1 and t.stride(0) != n * stride):
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} given, {dtype} {shape} needed")
+    B, n, heads, D = shape
+    s0, s1, s2, s3 = t.stride()
+    stride = s1 if n > 1 else s0 if B > 1 else heads * D
+    if s3 != 1 or (heads > 1 and s2 != D) or (B > 1 and s0 != n * stride):
         raise ValueError(f"{name}: head rows of a token must be contiguous and tokens evenly spaced")
-    _on_device(name, t)
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the call runs on device {dev}")
     return t.data_ptr(), stride
 
 
 def sik_rope_append(layout, chunk, q, k, q_out, *, v=None, k_out=None, K=None, V=None, q_weight=None, k_weight=None,
                     eps=1e-6, inv_freq=None, interleaved=False, positions=None):
     """Per-head norms and position rotation of q, k [B,n,heads,D]; keys (and values) into the cache, or keys to k_out."""
-    B, n, D = layout.batch, chunk.n, layout.head_dim
-    kd = _SIK2TORCH[layout.kv_dtype]
-    pages = _check_chunk(layout, chunk)
-    qp, qs = _head_rows("q", q, layout, n, layout.n_q_heads)
-    kp, ks = _head_rows("k", k, layout, n, layout.n_kv_heads)
-    vp, vs = (None, 0) if v is None else _head_rows("v", v, layout, n, layout.n_kv_heads)
-    st = _stream()
-    a = RopeArgs(qp, kp, vp, qs, ks, vs, _tensor("q_weight", q_weight, torch.float32, (D,), optional=True),
-                 _tensor("k_weight", k_weight, torch.float32, (D,), optional=True), float(eps),
-                 _tensor("inv_freq", inv_freq, torch.float32, optional=True),
-                 0 if inv_freq is None else 2 * inv_freq.numel(), 1 if interleaved else 0,
-                 _tensor("positions", positions, torch.int32, (B, n), optional=True),
-                 _tensor("q_out", q_out, kd, (B, n, layout.n_q_heads, D)),
-                 _tensor("k_out", k_out, kd, (B, n, layout.n_kv_heads, D), optional=True),
-                 _cache("K", K, layout, pages, optional=True), _cache("V", V, layout, pages, optional=True),
-                 None if st is None else st.value)
+    B, n, Hkv, Hq, D = layout.batch, chunk.n, layout.n_kv_heads, layout.n_q_heads, layout.head_dim
+    dev, kd, f32 = _device(), _SIK2TORCH[layout.kv_dtype], torch.float32
+    pages = _check_chunk(layout, chunk, dev)
+    q_rows, k_rows = (B, n, Hq, D), (B, n, Hkv, D)
+    qp, qs = _head_rows("q", q, kd, dev, q_rows)
+    kp, ks = _head_rows("k", k, kd, dev, k_rows)
+    vp, vs = (None, 0) if v is None else _head_rows("v", v, kd, dev, k_rows)
+    cache = _cache_shape(layout, pages)
+    a = RopeArgs(qp, kp, vp, qs, ks, vs, _tensor("q_weight", q_weight, f32, dev, (D,), optional=True),
+                 _tensor("k_weight", k_weight, f32, dev, (D,), optional=True), eps,
+                 _tensor("inv_freq", inv_freq, f32, dev, optional=True), 0 if inv_freq is None else 2 * inv_freq.numel(),
+                 1 if interleaved else 0, _tensor("positions", positions, torch.int32, dev, (B, n), optional=True),
+                 _tensor("q_out", q_out, kd, dev, q_rows), _tensor("k_out", k_out, kd, dev, k_rows, optional=True),
+                 _tensor("K", K, kd, dev, cache, optional=True), _tensor("V", V, kd, dev, cache, optional=True),
+                 _stream_of(dev))
     _check(lib().sik_rope_append(ctypes.byref(layout), ctypes.byref(chunk), ctypes.byref(a)))
 
 
@@ -440,49 +454,47 @@ def alloc_chunk_workspace(layout: Layout, n: int, device="cuda") -> torch.Tensor
     return torch.empty(size, dtype=torch.uint8, device=device)
 
 
-def _scratch(workspace):
-    return None if workspace is None else _tensor("workspace", workspace, torch.uint8)
-
-
 def sik_chunk_attn(layout, chunk, q, K, V, softmax_scale, out, lse, workspace):
     """Attention of the chunk's queries q [B,n,Hq,D] over the cache; lse [B,n,Hq] fp32 or None."""
-    rows = (layout.batch, chunk.n, layout.n_q_heads)
-    pages = _check_chunk(layout, chunk)
+    dev, kd = _device(), _SIK2TORCH[layout.kv_dtype]
+    rows = (layout.batch, chunk.n, layout.n_q_heads, layout.head_dim)
+    cache = _cache_shape(layout, _check_chunk(layout, chunk, dev))
     _check(lib().sik_chunk_attn(
-        ctypes.byref(layout), ctypes.byref(chunk), _tensor("q", q, _SIK2TORCH[layout.kv_dtype], (*rows, layout.head_dim)),
-        _cache("K", K, layout, pages), _cache("V", V, layout, pages), float(softmax_scale),
-        _tensor("out", out, _SIK2TORCH[layout.out_dtype], (*rows, layout.head_dim)),
-        _tensor("lse", lse, torch.float32, rows, optional=True), _scratch(workspace),
-        workspace.numel() if workspace is not None else 0, _stream()))
+        ctypes.byref(layout), ctypes.byref(chunk), _tensor("q", q, kd, dev, rows), _tensor("K", K, kd, dev, cache),
+        _tensor("V", V, kd, dev, cache), softmax_scale, _tensor("out", out, _SIK2TORCH[layout.out_dtype], dev, rows),
+        _tensor("lse", lse, torch.float32, dev, rows[:3], optional=True),
+        _tensor("workspace", workspace, torch.uint8, dev, optional=True),
+        workspace.numel() if workspace is not None else 0, _stream_of(dev)))
 
 
 def sik_attn_mass(layout, chunk, q, K, softmax_scale, lse, n_obs, before, mass):
     """Attention weight of the cached tokens from the last n_obs queries; before [B,Hkv,max_len] fp32 or None is added."""
-    rows = (layout.batch, chunk.n, layout.n_q_heads)
+    dev, kd, f32 = _device(), _SIK2TORCH[layout.kv_dtype], torch.float32
+    rows = (layout.batch, chunk.n, layout.n_q_heads, layout.head_dim)
     sums = (layout.batch, layout.n_kv_heads, layout.max_len)
-    pages = _check_chunk(layout, chunk)
+    cache = _cache_shape(layout, _check_chunk(layout, chunk, dev))
     _check(lib().sik_attn_mass(
-        ctypes.byref(layout), ctypes.byref(chunk), _tensor("q", q, _SIK2TORCH[layout.kv_dtype], (*rows, layout.head_dim)),
-        _cache("K", K, layout, pages), float(softmax_scale), _tensor("lse", lse, torch.float32, rows), int(n_obs),
-        _tensor("before", before, torch.float32, sums, optional=True), _tensor("mass", mass, torch.float32, sums),
-        _stream()))
+        ctypes.byref(layout), ctypes.byref(chunk), _tensor("q", q, kd, dev, rows), _tensor("K", K, kd, dev, cache),
+        softmax_scale, _tensor("lse", lse, f32, dev, rows[:3]), int(n_obs),
+        _tensor("before", before, f32, dev, sums, optional=True), _tensor("mass", mass, f32, dev, sums), _stream_of(dev)))
 
 
 def sik_evict(layout, mass, seq_len, n_keep, keep, workspace, *, n_sink=0, n_recent=0, new_len=None, K=None, V=None,
               pages=None, K_out=None, V_out=None, mass_out=None):
     """The n_keep tokens per (sequence, KV head) that stay, and with K_out and V_out the cache cut down to them."""
     B, H, D = layout.batch, layout.n_kv_heads, layout.head_dim
-    _check_page_table(layout, pages)
+    dev, kd, f32, i32 = _device(), _SIK2TORCH[layout.kv_dtype], torch.float32, torch.int32
+    n_keep = int(n_keep)
+    _check_page_table(layout, pages, dev)
     out_len = K_out.shape[2] if K_out is not None else mass_out.shape[2] if mass_out is not None else 0
-    kd, st = _SIK2TORCH[layout.kv_dtype], _stream()
-    a = EvictArgs(_tensor("mass", mass, torch.float32, (B, H, layout.max_len)),
-                  _tensor("seq_len", seq_len, torch.int32, numel=B), int(n_keep), int(n_sink), int(n_recent),
-                  _tensor("keep", keep, torch.int32, (B, H, int(n_keep))),
-                  _tensor("new_len", new_len, torch.int32, numel=B, optional=True),
-                  _cache("K", K, layout, pages, optional=True), _cache("V", V, layout, pages, optional=True),
-                  None if pages is None else ctypes.pointer(pages),
-                  _tensor("K_out", K_out, kd, (B, H, out_len, D), optional=True),
-                  _tensor("V_out", V_out, kd, (B, H, out_len, D), optional=True),
-                  _tensor("mass_out", mass_out, torch.float32, (B, H, out_len), optional=True), out_len,
-                  _scratch(workspace), workspace.numel() if workspace is not None else 0, None if st is None else st.value)
+    cache, cut = _cache_shape(layout, pages), (B, H, out_len, D)
+    a = EvictArgs(_tensor("mass", mass, f32, dev, (B, H, layout.max_len)), _tensor("seq_len", seq_len, i32, dev, numel=B),
+                  n_keep, int(n_sink), int(n_recent), _tensor("keep", keep, i32, dev, (B, H, n_keep)),
+                  _tensor("new_len", new_len, i32, dev, numel=B, optional=True),
+                  _tensor("K", K, kd, dev, cache, optional=True), _tensor("V", V, kd, dev, cache, optional=True),
+                  None if pages is None else ctypes.pointer(pages), _tensor("K_out", K_out, kd, dev, cut, optional=True),
+                  _tensor("V_out", V_out, kd, dev, cut, optional=True),
+                  _tensor("mass_out", mass_out, f32, dev, cut[:3], optional=True), out_len,
+                  _tensor("workspace", workspace, torch.uint8, dev, optional=True),
+                  workspace.numel() if workspace is not None else 0, _stream_of(dev))
     _check(lib().sik_evict(ctypes.byref(layout), ctypes.byref(a)))
