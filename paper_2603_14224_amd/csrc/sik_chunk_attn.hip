@@ -373,42 +373,60 @@ __global__ __launch_bounds__(kBlock, 2) void chunk_tokens_kernel(const ChunkAttn
     }
 }
 
-// The states of one row's parts, joined in their order: 32 lanes of four channels, eight parts at a time.
+// The states of one row's parts, joined in their order: a part per lane for the maxima and sums, then 32 lanes of four channels
+// and eight parts at a time for the outputs, all requested before the first is used.
 template <int ODT>
 __global__ __launch_bounds__(kBlock) void chunk_join_kernel(const ChunkAttn a, int tile_rows) {
-    __shared__ float s_sum[8];
-    __shared__ float4 s_o[8][32];
+    constexpr int kGroups = kBlock / 32, kEach = kMaxParts / kGroups;
+    __shared__ float s_f[kMaxParts];
+    __shared__ float4 s_o[kGroups][32];
     const int64_t row = blockIdx.x;  // of [unit][n * R]
     const int per = a.ch.n * a.R, u = static_cast<int>(row / per), m = static_cast<int>(row % per);
     const int b = u / a.cv.Hkv, h = u % a.cv.Hkv;
+    const int tid = threadIdx.x, lane = tid & 63, g = tid >> 5, c4 = tid & 31;
+    const int64_t p0 = (static_cast<int64_t>(u) * a.tiles + m / tile_rows) * a.parts;
     const int past = chunk_past(a.ch, b, a.cv.Lmax), nn = chunk_new(a.ch, b, past, a.cv.Lmax);
     if (m >= nn * a.R) return;
-    const int64_t p0 = (static_cast<int64_t>(u) * a.tiles + m / tile_rows) * a.parts;
-    const int tid = threadIdx.x, g = tid >> 5, c4 = tid & 31;
-    // (every wavefront of the workgroup reads all the maxima: no exchange needed for the largest)
-    float M = kNegBig;
-    float2 ml = make_float2(kNegBig, 0.0f);
-    for (int p = 0; p < a.parts; ++p)
-        M = fmaxf(M, reinterpret_cast<const float2*>(a.part_ml)[(p0 + p) * tile_rows + m % tile_rows].x);
-    float l = 0.0f;
+    // every wavefront takes the maxima and sums of all parts, two to a lane
+    float2 ml[kMaxParts / 64];
+    float M = kNegBig, l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kMaxParts / 64; ++i) {
+        const int p = lane + 64 * i;
+        ml[i] = p < a.parts ? reinterpret_cast<const float2*>(a.part_ml)[(p0 + p) * tile_rows + m % tile_rows]
+                            : make_float2(kNegBig, 0.0f);
+        M = fmaxf(M, ml[i].x);
+    }
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
+#pragma unroll
+    for (int i = 0; i < kMaxParts / 64; ++i) {
+        const float f = ml[i].y > 0.0f ? fast_exp2(ml[i].x - M) : 0.0f;  // a part without tokens has not written its rows
+        l += ml[i].y * f;
+        if (tid < 64) s_f[lane + 64 * i] = f;
+    }
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x, 64);
+    __syncthreads();
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int p = g; p < a.parts; p += 8) {
-        const int64_t at = (p0 + p) * tile_rows + m % tile_rows;
-        ml = reinterpret_cast<const float2*>(a.part_ml)[at];
-        if (ml.y <= 0.0f) continue;  // a part without tokens has not written its rows
-        const float f = fast_exp2(ml.x - M);
-        const float4 x = reinterpret_cast<const float4*>(a.part_o)[at * (kD / 4) + c4];
-        l += ml.y * f;
-        o.x += x.x * f, o.y += x.y * f, o.z += x.z * f, o.w += x.w * f;
+    for (int i0 = 0; i0 < kEach && i0 * kGroups < a.parts; i0 += 4) {
+        float4 x[4];
+        float f[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int p = g + kGroups * (i0 + i);
+            f[i] = p < a.parts ? s_f[p] : 0.0f;
+            x[i] = f[i] > 0.0f ? reinterpret_cast<const float4*>(a.part_o)[((p0 + p) * tile_rows + m % tile_rows) * (kD / 4) + c4]
+                               : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o.x += x[i].x * f[i], o.y += x[i].y * f[i], o.z += x[i].z * f[i], o.w += x[i].w * f[i];
     }
     s_o[g][c4] = o;
-    if (c4 == 0) s_sum[g] = l;
     __syncthreads();
     if (g != 0) return;
-    l = s_sum[0];
 #pragma unroll
-    for (int x = 1; x < 8; ++x) {
-        l += s_sum[x];
+    for (int x = 1; x < kGroups; ++x) {
         const float4 y = s_o[x][c4];
         o.x += y.x, o.y += y.y, o.z += y.z, o.w += y.w;
     }
