@@ -66,7 +66,8 @@ __device__ __forceinline__ void find_digit(const uint32_t (&c)[NB], uint32_t& di
     if (lane == 63) totals[wv] = incl;
     __syncthreads();
     uint32_t before = incl - mine;
-    for (int w = 0; w < wv; ++w) before += totals[w];
+#pragma unroll
+    for (int w = 0; w < BLOCK / kWave; ++w) before += w < wv ? totals[w] : 0u;
     if (before < need && need <= before + mine) {
 #pragma unroll
         for (int i = NB - 1; i >= 0; --i) {
@@ -115,11 +116,10 @@ __device__ __forceinline__ void before_wave(uint32_t a, uint32_t b, uint32_t (*t
         tot[wv][1] = b;
     }
     __syncthreads();
+#pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-        if (w < wv) {
-            ba += tot[w][0];
-            bb += tot[w][1];
-        }
+        ba += w < wv ? tot[w][0] : 0u;
+        bb += w < wv ? tot[w][1] : 0u;
     }
 }
 
@@ -192,68 +192,88 @@ struct EvictScratch {
     int64_t list_len;
 };
 
-__global__ __launch_bounds__(kBlock) void evict_count_kernel(EvictArgs a, int Hkv, int Lmax, EvictScratch w) {
+// A wavefront's consecutive part of a chunk, [first, last) in steps of 256 tokens, four per lane.  The first steps (all of them
+// where a chunk has kChunkTokens) are requested before anything else is known, lengths included, so that a launch waits for
+// memory once: a step's weights then come from registers however often they are looked at.
+struct PartWeights {
+    static constexpr int kHeld = kChunkTokens / (kEvictBlock / kWave) / 256;
+    const float* m;
+    int Lmax, lane, start, len, first, last;
+    f32x4_any held[kHeld];
+    __device__ __forceinline__ PartWeights(const float* mass, int Lmax_, const EvictScratch& w, int c) : m(mass), Lmax(Lmax_) {
+        len = w.per / (kEvictBlock / kWave);
+        lane = threadIdx.x & 63;
+        start = c * w.per + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * len;
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) held[k] = load4(m, start + 256 * k + 4 * lane, Lmax);
+    }
+    __device__ __forceinline__ void end_at(int L) {
+        first = min(start, L);
+        last = min(start + len, L);
+    }
+    // f(token, its weight and the three after it), every lane of the wavefront in every step
+    template <class F>
+    __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k)
+            if (first + 256 * k < last) f(first + 256 * k + 4 * lane, held[k]);
+        for (int i0 = first + 256 * kHeld; i0 < last; i0 += 256) f(i0 + 4 * lane, load4(m, i0 + 4 * lane, Lmax));
+    }
+};
+
+__global__ __launch_bounds__(kEvictBlock) void evict_count_kernel(EvictArgs a, int Hkv, int Lmax, EvictScratch w) {
     __shared__ uint32_t hist[kDigitBins];
     const int u = blockIdx.x / w.chunks, c = blockIdx.x % w.chunks;
+    PartWeights part(a.mass + static_cast<int64_t>(u) * Lmax, Lmax, w, c);
     const EvictRow r = evict_row(a, u / Hkv, Lmax);
-    if (r.L <= a.n_keep || r.need == 0) return;
-    for (int i = threadIdx.x; i < kDigitBins; i += kBlock) hist[i] = 0;
+    for (int i = threadIdx.x; i < kDigitBins; i += kEvictBlock) hist[i] = 0;
+    if (r.L <= a.n_keep || c * w.per >= r.L) return;
     __syncthreads();
-    const float* m = a.mass + static_cast<int64_t>(u) * Lmax;
-    const int end = min(r.L, (c + 1) * w.per);
-    for (int i0 = c * w.per; i0 < end; i0 += 4 * kBlock) {  // (the whole workgroup: the counting uses ballots)
-        const int i = i0 + 4 * static_cast<int>(threadIdx.x);
-        const f32x4_any v = load4(m, i, i < end ? r.L : 0);
+    part.end_at(r.L);
+    part.each([&](int i, f32x4_any v) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) count_bins(hist, float_to_key(v[e]) >> 21, i + e < end && r.inner(i + e));
-    }
+        for (int e = 0; e < 4; ++e) count_bins(hist, float_to_key(v[e]) >> 21, i + e < part.last && r.inner(i + e));
+    });
     __syncthreads();
-    uint32_t* out = w.counts + static_cast<int64_t>(blockIdx.x) * kDigitBins;
-    for (int i = threadIdx.x; i < kDigitBins; i += kBlock) out[i] = hist[i];
+    uint2* out = reinterpret_cast<uint2*>(w.counts + static_cast<int64_t>(blockIdx.x) * kDigitBins);
+    out[threadIdx.x] = reinterpret_cast<const uint2*>(hist)[threadIdx.x];
 }
 
-// A wavefront's quarter of a chunk: [first, last), in steps of 256 tokens, four per lane.
-__device__ __forceinline__ void quarter(const EvictScratch& w, const EvictRow& r, int c, int& first, int& last) {
-    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = ((w.per / 4 + 255) / 256) * 256;
-    const int end = min(r.L, (c + 1) * w.per);
-    first = min(c * w.per + wv * q, end);
-    last = min(first + q, end);
-}
-
-__global__ __launch_bounds__(kBlock) void evict_collect_kernel(EvictArgs a, int Hkv, int Lmax, EvictScratch w) {
-    constexpr int kWaves = kBlock / kWave, NB = kDigitBins / kBlock;
+__global__ __launch_bounds__(kEvictBlock) void evict_collect_kernel(EvictArgs a, int Hkv, int Lmax, EvictScratch w) {
+    constexpr int kWaves = kEvictBlock / kWave;
     __shared__ uint32_t totals[kWaves], found[2], s_before, s_list, s_len, s_tot[kWaves][2];
     const int tid = threadIdx.x, lane = tid & 63;
     const int u = blockIdx.x / w.chunks, c = blockIdx.x % w.chunks;
+    // counts of this thread's two bins over all chunks and over those before this one (chunks without tokens have not
+    // written theirs)
+    const uint32_t* cp = w.counts + static_cast<int64_t>(u) * w.chunks * kDigitBins + 2 * (kEvictBlock - 1 - tid);
+    constexpr int kAhead = 8;
+    uint2 x[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+        x[k] = k < w.chunks ? *reinterpret_cast<const uint2*>(cp + static_cast<int64_t>(k) * kDigitBins) : make_uint2(0u, 0u);
+    PartWeights part(a.mass + static_cast<int64_t>(u) * Lmax, Lmax, w, c);
     const EvictRow r = evict_row(a, u / Hkv, Lmax);
-    if (r.L <= a.n_keep || r.need == 0 || c * w.per >= r.L) return;
-    // counts of this thread's bins over all chunks and over those before this one
-    uint32_t all[NB], before[NB];
-#pragma unroll
-    for (int i = 0; i < NB; ++i) all[i] = before[i] = 0;
-    const uint32_t* cp = w.counts + static_cast<int64_t>(u) * w.chunks * kDigitBins + NB * (kBlock - 1 - tid);
+    if (r.L <= a.n_keep || c * w.per >= r.L) return;
+    part.end_at(r.L);
     const int used = (r.L + w.per - 1) / w.per;
+    uint32_t all[2] = {0u, 0u}, before[2] = {0u, 0u};
+    auto add = [&](int k, uint2 y) {
+        if (k >= used) return;
+        all[0] += y.x, all[1] += y.y;
+        if (k < c) before[0] += y.x, before[1] += y.y;
+    };
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) add(k, x[k]);
 #pragma unroll 4
-    for (int k = 0; k < used; ++k) {
-        uint32_t x[NB];
-#pragma unroll
-        for (int i = 0; i < NB; i += 4) {
-            const uint4 y = *reinterpret_cast<const uint4*>(cp + static_cast<int64_t>(k) * kDigitBins + i);
-            x[i] = y.x, x[i + 1] = y.y, x[i + 2] = y.z, x[i + 3] = y.w;
-        }
-#pragma unroll
-        for (int i = 0; i < NB; ++i) {
-            all[i] += x[i];
-            before[i] += k < c ? x[i] : 0u;
-        }
-    }
+    for (int k = kAhead; k < used; ++k) add(k, *reinterpret_cast<const uint2*>(cp + static_cast<int64_t>(k) * kDigitBins));
     if (tid == 0) s_before = 0;
     uint32_t bin, need = r.need;
-    find_digit<kBlock>(all, bin, need, totals, found);
+    find_digit<kEvictBlock>(all, bin, need, totals, found);
     uint32_t above = 0;
 #pragma unroll
-    for (int i = 0; i < NB; ++i) {
-        const uint32_t mine = NB * (kBlock - 1 - tid) + i;
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t mine = 2 * (kEvictBlock - 1 - tid) + i;
         if (mine > bin) above += before[i];
         if (mine == bin) {
             s_list = before[i];
@@ -263,94 +283,95 @@ __global__ __launch_bounds__(kBlock) void evict_collect_kernel(EvictArgs a, int 
     above = wave_sum(above);
     if (lane == 0 && above) atomicAdd(&s_before, above);
     // the tokens of that bin, in order
-    int first, last;
-    quarter(w, r, c, first, last);
-    const float* m = a.mass + static_cast<int64_t>(u) * Lmax;
+    auto in_bin = [&](int i, float v) { return i < part.last && r.inner(i) && float_to_key(v) >> 21 == bin; };
     uint32_t n = 0;
-    for (int i0 = first; i0 < last; i0 += 256) {
-        const int i = i0 + 4 * lane;
-        const f32x4_any v = load4(m, i, i < last ? r.L : 0);
+    part.each([&](int i, f32x4_any v) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) n += __popcll(__ballot(i + e < last && r.inner(i + e) && float_to_key(v[e]) >> 21 == bin));
-    }
+        for (int e = 0; e < 4; ++e) n += __popcll(__ballot(in_bin(i + e, v[e])));
+    });
     uint32_t at = 0, none = 0;
     before_wave<kWaves>(n, 0u, s_tot, at, none);
     at += s_list;
     if (tid == 0) {
         const int cs = c * w.per;  // kept ends in front of the chunk stay as well
-        uint32_t* hd = w.heads + static_cast<int64_t>(blockIdx.x) * 4;
-        hd[0] = s_list;
-        hd[1] = s_before + min(cs, r.lo) + max(0, cs - max(r.hi, r.lo));
-        hd[2] = s_len;
-        hd[3] = need;
+        reinterpret_cast<uint4*>(w.heads)[blockIdx.x] =
+            make_uint4(s_list, s_before + min(cs, r.lo) + max(0, cs - max(r.hi, r.lo)), s_len, need);
         if (c == 0) w.bins[u] = bin;
     }
     uint32_t* list = w.list + u * w.list_len;
-    for (int i0 = first; i0 < last; i0 += 256) {
-        const int i = i0 + 4 * lane;
-        const f32x4_any v = load4(m, i, i < last ? r.L : 0);
+    part.each([&](int i, f32x4_any v) {
         bool in[4];
         uint32_t k = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            in[e] = i + e < last && r.inner(i + e) && float_to_key(v[e]) >> 21 == bin;
+            in[e] = in_bin(i + e, v[e]);
             k += in[e];
         }
+        if (__ballot(k != 0) == 0) return;
         const uint32_t incl = wave_inclusive_sum(k);
         uint32_t p = at + incl - k;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (in[e]) list[p++] = float_to_key(v[e]);
         at += __builtin_amdgcn_readlane(incl, 63);
-    }
+    });
 }
 
-__global__ __launch_bounds__(kBlock) void evict_place_kernel(EvictArgs a, int Hkv, int Lmax, EvictScratch w) {
-    constexpr int kWaves = kBlock / kWave, NB = kDigitBins / kBlock;
+__global__ __launch_bounds__(kEvictBlock) void evict_place_kernel(EvictArgs a, int Hkv, int Lmax, EvictScratch w) {
+    constexpr int kWaves = kEvictBlock / kWave, kListed = 4;
     __shared__ uint32_t hist[kDigitBins];
     __shared__ uint32_t totals[kWaves], found[2], s_sure, s_equal, s_tot[kWaves][2];
     const int tid = threadIdx.x, lane = tid & 63;
-    const int u = blockIdx.x / w.chunks, c = blockIdx.x % w.chunks;
+    const int u = blockIdx.x / w.chunks, c = blockIdx.x % w.chunks, cs = c * w.per;
+    const bool any = a.n_sink + a.n_recent < a.n_keep;
+    // the front of the list, long enough for most rows, is requested with the weights (what lies behind its end is not used)
+    const uint32_t* list = w.list + u * w.list_len;
+    uint32_t listed[kListed];
+#pragma unroll
+    for (int k = 0; k < kListed; ++k) listed[k] = any && k * kEvictBlock + tid < w.list_len ? list[k * kEvictBlock + tid] : 0u;
+    uint4 hd = make_uint4(0u, 0u, 0u, 0u);
+    uint32_t cut = 0;
+    if (any) {
+        hd = reinterpret_cast<const uint4*>(w.heads)[blockIdx.x];
+        cut = w.bins[u];
+    }
+    PartWeights part(a.mass + static_cast<int64_t>(u) * Lmax, Lmax, w, c);
     const EvictRow r = evict_row(a, u / Hkv, Lmax);
     int32_t* keep = a.keep + static_cast<int64_t>(u) * a.n_keep;
     if (a.new_len && u % Hkv == 0 && c == 0 && tid == 0) a.new_len[u / Hkv] = min(r.L, a.n_keep);
-    const int cs = c * w.per;
     if (r.L <= a.n_keep) {
-        for (int i = cs + tid; i < min(a.n_keep, cs + w.per); i += kBlock) keep[i] = i < r.L ? i : -1;
+        for (int i = cs + tid; i < min(a.n_keep, cs + w.per); i += kEvictBlock) keep[i] = i < r.L ? i : -1;
         return;
     }
     if (cs >= r.L) return;
-    uint32_t cut = 0, need = 0, sure0, equal0 = 0;
-    const bool any = r.need > 0;
+    part.end_at(r.L);
+    uint32_t need = hd.w, sure0 = hd.y, equal0 = 0;
     if (any) {
-        const uint32_t* hd = w.heads + static_cast<int64_t>(blockIdx.x) * 4;
-        const uint32_t mine = hd[0], len = hd[2];
-        sure0 = hd[1];
-        need = hd[3];
-        cut = w.bins[u];
-        const uint32_t* list = w.list + u * w.list_len;
+        const uint32_t mine = hd.x, len = hd.z;
+        auto each = [&](uint32_t n, auto f) {  // f(key, place < n), every lane of the wavefront in every step
+#pragma unroll
+            for (uint32_t k = 0; k < kListed; ++k)
+                if (k * kEvictBlock < n) f(listed[k], k * kEvictBlock + tid < n);
+            for (uint32_t p = kListed * kEvictBlock; p < n; p += kEvictBlock) f(p + tid < n ? list[p + tid] : 0u, p + tid < n);
+        };
         if (tid == 0) s_sure = s_equal = 0;
         for (int digit = 1; digit < 3; ++digit) {
-            for (int i = tid; i < kDigitBins; i += kBlock) hist[i] = 0;
+            hist[tid] = hist[tid + kEvictBlock] = 0;
             __syncthreads();
-            for (uint32_t p = 0; p < len; p += kBlock) {
-                const uint32_t key = p + tid < len ? list[p + tid] : 0u;
-                count_bins(hist, digit == 1 ? (key >> 10) & 2047u : key & 1023u,
-                           p + tid < len && (digit == 1 || key >> 10 == cut));
-            }
+            each(len, [&](uint32_t key, bool on) {
+                count_bins(hist, digit == 1 ? (key >> 10) & 2047u : key & 1023u, on && (digit == 1 || key >> 10 == cut));
+            });
             __syncthreads();
-            uint32_t x[NB], d;
-#pragma unroll
-            for (int i = 0; i < NB; ++i) x[i] = hist[NB * (kBlock - 1 - tid) + i];
-            find_digit<kBlock>(x, d, need, totals, found);
+            const uint32_t x[2] = {hist[2 * (kEvictBlock - 1 - tid)], hist[2 * (kEvictBlock - 1 - tid) + 1]};
+            uint32_t d;
+            find_digit<kEvictBlock>(x, d, need, totals, found);
             cut = cut << (digit == 1 ? 11 : 10) | d;
         }
         uint32_t ns = 0, ne = 0;  // of the list's tokens in front of the chunk
-        for (uint32_t p = tid; p < mine; p += kBlock) {
-            const uint32_t key = list[p];
-            ns += key > cut;
-            ne += key == cut;
-        }
+        each(mine, [&](uint32_t key, bool on) {
+            ns += on && key > cut;
+            ne += on && key == cut;
+        });
         ns = wave_sum(ns);
         ne = wave_sum(ne);
         if (lane == 0 && (ns | ne)) {
@@ -363,35 +384,27 @@ __global__ __launch_bounds__(kBlock) void evict_place_kernel(EvictArgs a, int Hk
     } else {
         sure0 = min(cs, r.lo) + max(0, cs - max(r.hi, r.lo));
     }
-    int first, last;
-    quarter(w, r, c, first, last);
-    const float* m = a.mass + static_cast<int64_t>(u) * Lmax;
-    auto classes = [&](int i, bool (&sure)[4], bool (&equal)[4]) {
-        const f32x4_any v = load4(m, i, i < last ? r.L : 0);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t key = float_to_key(v[e]);
-            sure[e] = i + e < last && (!r.inner(i + e) || (any && key > cut));
-            equal[e] = any && i + e < last && r.inner(i + e) && key == cut;
-        }
-    };
+    auto sure_of = [&](int i, float v) { return i < part.last && (!r.inner(i) || (any && float_to_key(v) > cut)); };
+    auto equal_of = [&](int i, float v) { return any && i < part.last && r.inner(i) && float_to_key(v) == cut; };
     uint32_t ns = 0, ne = 0;
-    for (int i0 = first; i0 < last; i0 += 256) {
-        bool sure[4], equal[4];
-        classes(i0 + 4 * lane, sure, equal);
+    part.each([&](int i, f32x4_any v) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            ns += __popcll(__ballot(sure[e]));
-            ne += __popcll(__ballot(equal[e]));
+            ns += __popcll(__ballot(sure_of(i + e, v[e])));
+            ne += __popcll(__ballot(equal_of(i + e, v[e])));
         }
-    }
+    });
     uint32_t ps = sure0, pe = equal0;
     before_wave<kWaves>(ns, ne, s_tot, ps, pe);
-    for (int i0 = first; i0 < last; i0 += 256) {
+    part.each([&](int i, f32x4_any v) {
         bool sure[4], equal[4];
-        classes(i0 + 4 * lane, sure, equal);
-        place4(keep, i0 + 4 * lane, sure, equal, need, ps, pe);
-    }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            sure[e] = sure_of(i + e, v[e]);
+            equal[e] = equal_of(i + e, v[e]);
+        }
+        place4(keep, i, sure, equal, need, ps, pe);
+    });
 }
 
 // 16 lanes copy a kept row of K and of V, kRowsEach of them, all requested before the first is stored.
@@ -432,13 +445,13 @@ static EvictScratch evict_plan(const Dims& d, void* ws, size_t* bytes) {
     EvictScratch w{};
     w.per = kChunkTokens;
     const int least = (d.Lmax + kEvictChunks - 1) / kEvictChunks;
-    if (least > w.per) w.per = (least + 1023) / 1024 * 1024;
+    if (least > w.per) w.per = (least + 4095) / 4096 * 4096;
     w.chunks = d.Lmax <= kEvictDirect ? 0 : (d.Lmax + w.per - 1) / w.per;
     w.list_len = d.Lmax;
     const int64_t units = d.units(), rows = units * w.chunks;
     uint32_t* p = static_cast<uint32_t*>(ws);
     w.counts = p;
-    w.heads = w.counts + rows * kDigitBins;
+    w.heads = w.counts + rows * kDigitBins;  // (16-byte entries behind a multiple of 8 KB)
     w.bins = w.heads + rows * 4;
     w.list = w.bins + units;
     *bytes = w.chunks ? static_cast<size_t>(rows * (kDigitBins + 4) + units + units * w.list_len) * 4 : 0;
@@ -457,7 +470,7 @@ hipError_t launch_evict(const Dims& d, const CacheView& c, const EvictArgs& a, v
     const int nblk = (a.n_keep + kBlock / 16 * kRowsEach - 1) / (kBlock / 16 * kRowsEach);
     const bool rows = a.K_out || a.mass_out;
     const int64_t chunks = static_cast<int64_t>(w.chunks) * d.units();
-    if (chunks > 0x7fffffff / kBlock || d.units() > 0x7fffffff / kEvictBlock ||
+    if (chunks > 0x7fffffff / kEvictBlock || d.units() > 0x7fffffff / kEvictBlock ||
         (rows && static_cast<int64_t>(nblk) * d.units() > 0x7fffffff / kBlock))
         return hipErrorInvalidConfiguration;
     hipError_t e;
@@ -467,10 +480,10 @@ hipError_t launch_evict(const Dims& d, const CacheView& c, const EvictArgs& a, v
         const int grid = static_cast<int>(chunks);
         e = hipSuccess;
         if (a.n_sink + a.n_recent < a.n_keep) {
-            e = launch_kernel(evict_count_kernel, grid, kBlock, s, a, d.Hkv, d.Lmax, w);
-            if (e == hipSuccess) e = launch_kernel(evict_collect_kernel, grid, kBlock, s, a, d.Hkv, d.Lmax, w);
+            e = launch_kernel(evict_count_kernel, grid, kEvictBlock, s, a, d.Hkv, d.Lmax, w);
+            if (e == hipSuccess) e = launch_kernel(evict_collect_kernel, grid, kEvictBlock, s, a, d.Hkv, d.Lmax, w);
         }
-        if (e == hipSuccess) e = launch_kernel(evict_place_kernel, grid, kBlock, s, a, d.Hkv, d.Lmax, w);
+        if (e == hipSuccess) e = launch_kernel(evict_place_kernel, grid, kEvictBlock, s, a, d.Hkv, d.Lmax, w);
     }
     if (e != hipSuccess || !rows) return e;
     return launch_kernel(evict_rows_kernel, nblk * d.units(), kBlock, s, a, c, nblk);

@@ -1,14 +1,16 @@
 // Attention weight that each cached token receives from the last queries of a chunk.
 //
 // A wavefront owns 32 tokens: their keys stay in its registers as the second operand, the queries pass by as the first, 32
-// rows at a time through LDS (loaded one tile ahead, shared by the four wavefronts of a workgroup).  A lane then has one token
+// rows at a time through LDS (three tiles ahead, shared by the four wavefronts of a workgroup).  A lane then has one token
 // (column l % 32) and half of the tile's queries in its registers, so the weights are summed in the lane: no exchange, no
 // atomics, one order of additions.  Rows as in chunk attention: token t of the chunk and head r of the group are row t R + r.
 #include "sik_mma.h"
 
 namespace sik {
 
-constexpr int kMassRows = 32;
+constexpr int kMassRows = 32;    // query rows of a tile
+constexpr int kMassBuffers = 4;  // tiles in LDS
+constexpr int kMassStage = 512;  // rows whose sums are in LDS at a time
 
 struct MassArgs {
     const uint16_t *q, *K;
@@ -24,9 +26,9 @@ struct MassArgs {
 template <int DT>
 __global__ __launch_bounds__(kBlock, 4) void mass_kernel(const MassArgs a) {
     __shared__ struct {
-        __align__(16) char q[2][kMassRows * 256];
-        __align__(16) float lse[2][kMassRows];  // in powers of two; +infinity: the row contributes nothing
-        __align__(16) int last[2][kMassRows];   // last token that the row attends
+        __align__(16) char q[kMassBuffers][kMassRows * 256];
+        __align__(16) float lse[kMassStage];  // in powers of two; +infinity: the row contributes nothing
+        __align__(16) int last[kMassStage];   // last token that the row attends
     } lds;
     const int lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
     const int u = blockIdx.x / a.blocks, b = u / a.cv.Hkv, h = u % a.cv.Hkv;
@@ -48,53 +50,77 @@ __global__ __launch_bounds__(kBlock, 4) void mass_kernel(const MassArgs a) {
     const int m0 = t_begin * a.R, rows = nn * a.R;
     const int tiles = t_begin < nn ? (rows - m0 + kMassRows - 1) / kMassRows : 0;
     const int64_t chunk_row = static_cast<int64_t>(b) * a.ch.n;
-    // this lane's two rows of the loads (8 wv + 4 i + lane / 16 of a tile) and the first wavefront's row of the sums
-    auto load = [&](int tile, int buf, float& l, int& last) {
-        const int first = m0 + tile * kMassRows, t_first = first / a.R;
-        const uint16_t* base = uniform(a.q + ((chunk_row + t_first) * a.Hq + h * a.R) * kD);
+    // (token, head) of the next tile's first row and of this lane's two rows of its loads (8 wv + 4 i + lane / 16); 32 rows on
+    // is a fixed step with at most one carry, no division
+    const int step_t = kMassRows / a.R, step_r = kMassRows % a.R;
+    int ft = t_begin, fr = 0, lt[2], lr[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = 8 * wv + 4 * i + (lane >> 4);
+        lt[i] = t_begin + r / a.R;
+        lr[i] = r % a.R;
+    }
+    auto advance = [&](int& t, int& r) {
+        t += step_t;
+        r += step_r;
+        if (r >= a.R) {
+            r -= a.R;
+            ++t;
+        }
+    };
+    auto load = [&](int tile) {
+        char* to = lds.q[tile % kMassBuffers];
+        const uint16_t* base = uniform(a.q + ((chunk_row + ft) * a.Hq + h * a.R) * kD);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int r = 8 * wv + 4 * i + (lane >> 4), m = min(first + r, rows - 1), t = m / a.R;
-            const uint32_t off = (static_cast<uint32_t>(t - t_first) * a.Hq + (m - t * a.R)) * 256u +
-                                 (((lane & 15) ^ key_swizzle(r)) << 4);
-            dma_16(base, off, uniform(static_cast<int>(lds_offset(lds.q[buf]) + (8 * wv + 4 * i) * 256)));
+            const int row = 8 * wv + 4 * i + (lane >> 4);
+            const bool in = lt[i] < nn;  // rows beyond the end repeat the last one
+            const uint32_t off = (static_cast<uint32_t>((in ? lt[i] : nn - 1) - ft) * a.Hq + (in ? lr[i] : a.R - 1)) * 256u;
+            dma_16(base, off + (((lane & 15) ^ key_swizzle(row)) << 4),
+                   uniform(static_cast<int>(lds_offset(to) + (8 * wv + 4 * i) * 256)));
+            advance(lt[i], lr[i]);
         }
-        if (wv == 0 && lane < kMassRows) {
-            const int m = first + lane, t = m / a.R;
-            l = __builtin_inff();
-            last = past + t;
+        advance(ft, fr);
+    };
+    auto stage = [&](int tile) {  // sums and last tokens of the next kMassStage rows
+        for (int i = threadIdx.x; i < kMassStage; i += kBlock) {
+            const int m = m0 + tile * kMassRows + i, t = m / a.R;
+            float l = __builtin_inff();
             if (m < rows) {
                 const float x = a.lse[(chunk_row + t) * a.Hq + h * a.R + (m - t * a.R)];
                 if (x > -__builtin_inff()) l = x * 1.4426950408889634f;
             }
+            lds.lse[i] = l;
+            lds.last[i] = past + t;
         }
     };
-    auto publish = [&](int buf, float l, int last) {
-        if (wv == 0 && lane < kMassRows) {
-            lds.lse[buf][lane] = l;
-            lds.last[buf][lane] = last;
-        }
-    };
-    float l = 0.0f, sum = 0.0f;
-    int last = 0;
-    if (tiles > 0) {
-        load(0, 0, l, last);
-        publish(0, l, last);
-    }
+    float sum = 0.0f;
+    int first_t = t_begin, first_r = 0;
+#pragma unroll
+    for (int i = 0; i < kMassBuffers - 1; ++i)
+        if (i < tiles) load(i);
     for (int tile = 0; tile < tiles; ++tile) {
-        const int buf = tile & 1;
-        dma_wait<0>();
+        const int row0 = (tile * kMassRows) % kMassStage;
+        if (row0 == 0) {
+            if (tile) __syncthreads();  // the sums staged before have been read
+            stage(tile);
+        }
+        if (tile + kMassBuffers - 1 <= tiles)  // two newer tiles of two loads each are on their way
+            dma_wait<2 * (kMassBuffers - 2)>();
+        else
+            dma_wait<0>();
         lds_reads_done();
         barrier_only();
-        const bool more = tile + 1 < tiles;
-        if (more) load(tile + 1, buf ^ 1, l, last);
+        if (tile + kMassBuffers - 1 < tiles) load(tile + kMassBuffers - 1);
+        const char* qt = lds.q[tile % kMassBuffers];
         f32x16 s{};
 #pragma unroll
-        for (int step = 0; step < 8; ++step) s = mma32<DT>(row_fragment(lds.q[buf], lane, step), kf[step], s);
-        if (key0 + 32 * wv + 31 > past + (m0 + tile * kMassRows) / a.R) {
+        for (int step = 0; step < 8; ++step) s = mma32<DT>(row_fragment(qt, lane, step), kf[step], s);
+        const int at = row0 + 4 * (lane >> 5);
+        if (key0 + 32 * wv + 31 > past + first_t) {
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const int4 x = *reinterpret_cast<const int4*>(&lds.last[buf][8 * g + 4 * (lane >> 5)]);
+                const int4 x = *reinterpret_cast<const int4*>(&lds.last[at + 8 * g]);
                 s[4 * g] = key > x.x ? -__builtin_inff() : s[4 * g];
                 s[4 * g + 1] = key > x.y ? -__builtin_inff() : s[4 * g + 1];
                 s[4 * g + 2] = key > x.z ? -__builtin_inff() : s[4 * g + 2];
@@ -104,12 +130,12 @@ __global__ __launch_bounds__(kBlock, 4) void mass_kernel(const MassArgs a) {
         float part = 0.0f;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const float4 x = *reinterpret_cast<const float4*>(&lds.lse[buf][8 * g + 4 * (lane >> 5)]);
+            const float4 x = *reinterpret_cast<const float4*>(&lds.lse[at + 8 * g]);
             part += (fast_exp2(fmaf(s[4 * g], a.scale_log2e, -x.x)) + fast_exp2(fmaf(s[4 * g + 1], a.scale_log2e, -x.y))) +
                     (fast_exp2(fmaf(s[4 * g + 2], a.scale_log2e, -x.z)) + fast_exp2(fmaf(s[4 * g + 3], a.scale_log2e, -x.w)));
         }
         sum += part;
-        if (more) publish(buf ^ 1, l, last);
+        advance(first_t, first_r);
     }
     float lo, hi;
     both_halves(sum, lo, hi);
