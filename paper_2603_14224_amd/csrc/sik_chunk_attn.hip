@@ -31,7 +31,7 @@ struct ChunkAttn {
     float scale_log2e;
     void* out;
     float* lse;
-    float* part_o;   // [unit][tile][part][rows][kD]
+    float* part_o;   // [unit][tile][part] states: `tokens` form [32 rows][kD]; `rows` form [4 wavefronts] register by register
     float* part_ml;  // [unit][tile][part][rows][2]
 };
 
@@ -230,8 +230,8 @@ __global__ __launch_bounds__(kBlock, 2) void chunk_rows_kernel(const ChunkAttn a
     float lo, hi;
     both_halves(st.l, lo, hi);
     const float l = lo + hi;
-    if (w0 + (lane & 31) >= rows) return;
     if (a.parts == 1) {
+        if (w0 + (lane & 31) >= rows) return;
         const float inv = l > 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
         for (int c = 0; c < 4; ++c)
@@ -242,14 +242,16 @@ __global__ __launch_bounds__(kBlock, 2) void chunk_rows_kernel(const ChunkAttn a
         if (a.lse && lane < 32) a.lse[qrow] = log_sum(st.m, l);
         return;
     }
-    const int64_t pr = ((static_cast<int64_t>(pl.unit) * a.tiles + pl.tile) * a.parts + pl.part) * kRowsTile + 32 * wv + (lane & 31);
-    if (lane < 32) reinterpret_cast<float2*>(a.part_ml)[pr] = make_float2(st.m, l);
+    if (w0 >= rows) return;
+    // (four registers of all lanes at a time, 1 KB each: whole lines, whereas a row's 16 B would be pieces of 32 of them)
+    const int64_t pr = ((static_cast<int64_t>(pl.unit) * a.tiles + pl.tile) * a.parts + pl.part) * kRowsTile + 32 * wv;
+    if (lane < 32) reinterpret_cast<float2*>(a.part_ml)[pr + lane] = make_float2(st.m, l);
     if (t0 < t1) {
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
-                store4<kF32>(a.part_o, pr * kD + 32 * c + 2 * i + 4 * (lane >> 5), st.o[c][i], st.o[c][i + 1], st.o[c][i + 2],
+                store4<kF32>(a.part_o, pr * kD + ((4 * c + i / 4) * 64 + lane) * 4, st.o[c][i], st.o[c][i + 1], st.o[c][i + 2],
                              st.o[c][i + 3]);
     }
 }
@@ -373,10 +375,10 @@ __global__ __launch_bounds__(kBlock, 2) void chunk_tokens_kernel(const ChunkAttn
     }
 }
 
-// The states of one row's parts, joined in their order: a part per lane for the maxima and sums, then 32 lanes of four channels
+// The states of a row's parts, joined in their order.  After the `tokens` form a workgroup per row: a part per lane for the maxima and sums, then 32 lanes of four channels
 // and eight parts at a time for the outputs, all requested before the first is used.
 template <int ODT>
-__global__ __launch_bounds__(kBlock) void chunk_join_kernel(const ChunkAttn a, int tile_rows) {
+__global__ __launch_bounds__(kBlock) void join_tokens_kernel(const ChunkAttn a) {
     constexpr int kGroups = kBlock / 32, kEach = kMaxParts / kGroups;
     __shared__ float s_f[kMaxParts];
     __shared__ float4 s_o[kGroups][32];
@@ -384,7 +386,7 @@ __global__ __launch_bounds__(kBlock) void chunk_join_kernel(const ChunkAttn a, i
     const int per = a.ch.n * a.R, u = static_cast<int>(row / per), m = static_cast<int>(row % per);
     const int b = u / a.cv.Hkv, h = u % a.cv.Hkv;
     const int tid = threadIdx.x, lane = tid & 63, g = tid >> 5, c4 = tid & 31;
-    const int64_t p0 = (static_cast<int64_t>(u) * a.tiles + m / tile_rows) * a.parts;
+    const int64_t p0 = (static_cast<int64_t>(u) * a.tiles + m / kTokensTile) * a.parts;
     const int past = chunk_past(a.ch, b, a.cv.Lmax), nn = chunk_new(a.ch, b, past, a.cv.Lmax);
     if (m >= nn * a.R) return;
     // every wavefront takes the maxima and sums of all parts, two to a lane
@@ -393,7 +395,7 @@ __global__ __launch_bounds__(kBlock) void chunk_join_kernel(const ChunkAttn a, i
 #pragma unroll
     for (int i = 0; i < kMaxParts / 64; ++i) {
         const int p = lane + 64 * i;
-        ml[i] = p < a.parts ? reinterpret_cast<const float2*>(a.part_ml)[(p0 + p) * tile_rows + m % tile_rows]
+        ml[i] = p < a.parts ? reinterpret_cast<const float2*>(a.part_ml)[(p0 + p) * kTokensTile + m % kTokensTile]
                             : make_float2(kNegBig, 0.0f);
         M = fmaxf(M, ml[i].x);
     }
@@ -416,7 +418,7 @@ __global__ __launch_bounds__(kBlock) void chunk_join_kernel(const ChunkAttn a, i
         for (int i = 0; i < 4; ++i) {
             const int p = g + kGroups * (i0 + i);
             f[i] = p < a.parts ? s_f[p] : 0.0f;
-            x[i] = f[i] > 0.0f ? reinterpret_cast<const float4*>(a.part_o)[((p0 + p) * tile_rows + m % tile_rows) * (kD / 4) + c4]
+            x[i] = f[i] > 0.0f ? reinterpret_cast<const float4*>(a.part_o)[((p0 + p) * kTokensTile + m % kTokensTile) * (kD / 4) + c4]
                                : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
 #pragma unroll
@@ -434,6 +436,77 @@ __global__ __launch_bounds__(kBlock) void chunk_join_kernel(const ChunkAttn a, i
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
     store4<ODT>(a.out, at * kD + 4 * c4, o.x * inv, o.y * inv, o.z * inv, o.w * inv);
     if (a.lse && c4 == 0) a.lse[at] = log_sum(M, l);
+}
+
+// After the `rows` form: a lane has a row and four of its channels, as the states lie in memory.  SPLIT: the 8 groups of 32
+// lanes of a workgroup share one such block's parts (many parts, few rows), otherwise each has a block of its own.
+template <int ODT, bool SPLIT>
+__global__ __launch_bounds__(kBlock) void join_rows_kernel(const ChunkAttn a, int blocks) {
+    constexpr int kGroups = kBlock / 32, kEach = SPLIT ? kMaxParts / kGroups : kGroups;
+    __shared__ float s_m[kGroups][32], s_l[kGroups][32];
+    __shared__ float4 s_o[kGroups][32];
+    const int r = threadIdx.x & 31, g = threadIdx.x >> 5;
+    constexpr int kPer = SPLIT ? 32 : 32 / kGroups;  // workgroups to 32 rows
+    const int x = SPLIT ? blockIdx.x % kPer : blockIdx.x % kPer * kGroups + g;  // channels 32 (x / 8) + 8 (x % 8 / 2) + 4 (x % 2) ..
+    const int64_t w = blockIdx.x / kPer;  // 32 rows: [unit][block]
+    const int u = static_cast<int>(w / blocks), m = static_cast<int>(w % blocks) * 32 + r;
+    const int b = u / a.cv.Hkv, h = u % a.cv.Hkv;
+    const int past = chunk_past(a.ch, b, a.cv.Lmax), nn = chunk_new(a.ch, b, past, a.cv.Lmax), rows = nn * a.R;
+    if (m - r >= rows) return;
+    const int64_t p0 = (static_cast<int64_t>(u) * a.tiles + m / kRowsTile) * a.parts;
+    float2 ml[kEach];
+    float M = kNegBig, l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int p = SPLIT ? g + kGroups * i : i;
+        ml[i] = p < a.parts ? reinterpret_cast<const float2*>(a.part_ml)[(p0 + p) * kRowsTile + m % kRowsTile]
+                            : make_float2(kNegBig, 0.0f);
+        if (ml[i].y > 0.0f) M = fmaxf(M, ml[i].x);
+    }
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const float4* po = reinterpret_cast<const float4*>(a.part_o) +
+                       (p0 * kRowsTile + (m % kRowsTile - r)) * (kD / 4) + (x >> 1) * 64 + (x & 1) * 32 + r;
+#pragma unroll
+    for (int i0 = 0; i0 < kEach; i0 += 4) {
+        if ((SPLIT ? kGroups * i0 : i0) >= a.parts) break;
+        float4 y[4];
+        float f[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int p = SPLIT ? g + kGroups * (i0 + i) : i0 + i;
+            const bool on = ml[i0 + i].y > 0.0f;  // a part without tokens has not written its state
+            f[i] = on ? fast_exp2(ml[i0 + i].x - M) : 0.0f;
+            y[i] = on ? po[static_cast<int64_t>(p) * kRowsTile * (kD / 4)] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            l += ml[i0 + i].y * f[i];
+            o.x += y[i].x * f[i], o.y += y[i].y * f[i], o.z += y[i].z * f[i], o.w += y[i].w * f[i];
+        }
+    }
+    if constexpr (SPLIT) {
+        s_m[g][r] = M;
+        s_l[g][r] = l;
+        s_o[g][r] = o;
+        __syncthreads();
+        if (g != 0) return;
+#pragma unroll
+        for (int k = 1; k < kGroups; ++k) M = fmaxf(M, s_m[k][r]);
+        l = 0.0f;
+        o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int k = 0; k < kGroups; ++k) {
+            const float f = fast_exp2(s_m[k][r] - M);
+            const float4 y = s_o[k][r];
+            l += s_l[k][r] * f;
+            o.x += y.x * f, o.y += y.y * f, o.z += y.z * f, o.w += y.w * f;
+        }
+    }
+    if (m >= rows) return;
+    const int64_t at = (static_cast<int64_t>(b) * a.ch.n + m / a.R) * a.Hq + h * a.R + m % a.R;
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    store4<ODT>(a.out, at * kD + 32 * (x >> 3) + 8 * ((x & 7) >> 1) + 4 * (x & 1), o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    if (a.lse && x == 0) a.lse[at] = log_sum(M, l);
 }
 
 // Form and split of a call.  The `rows` form runs two workgroups to a compute unit, as does the `tokens` form.
@@ -456,6 +529,13 @@ static ChunkPlan chunk_plan(const Dims& d, int n) {
     return p;
 }
 
+static int join_blocks(const Dims& d, int n) { return static_cast<int>((static_cast<int64_t>(n) * d.R + 31) / 32); }
+static bool join_splits(const ChunkPlan& p) { return p.parts > 8; }
+static int64_t join_grid(const Dims& d, const ChunkPlan& p, int n) {
+    if (p.tokens) return static_cast<int64_t>(d.rows()) * n;
+    return static_cast<int64_t>(d.units()) * join_blocks(d, n) * (join_splits(p) ? 32 : 4);
+}
+
 static size_t plan_rows(const Dims& d, const ChunkPlan& p) {
     return p.parts == 1 ? 0 : static_cast<size_t>(d.units()) * p.tiles * p.parts * p.tile_rows;
 }
@@ -473,8 +553,10 @@ size_t chunk_attn_bytes(const Dims& d, int n) {
 
 hipError_t launch_chunk_attn(const Dims& d, const CacheView& c, const ChunkView& ch, const void* q, const void* K,
                              const void* V, float scale, void* out, float* lse, void* ws, hipStream_t s) {
+    if (static_cast<int64_t>(ch.n) * d.R > 0x7fffffff - kRowsTile) return hipErrorInvalidConfiguration;  // rows are counted in 32 bits
     const ChunkPlan p = chunk_plan(d, ch.n);
-    const int64_t grid = static_cast<int64_t>(d.units()) * p.tiles * p.parts, join = static_cast<int64_t>(d.rows()) * ch.n;
+    const int64_t grid = static_cast<int64_t>(d.units()) * p.tiles * p.parts, join = join_grid(d, p, ch.n);
+    const int blocks = join_blocks(d, ch.n);
     if (grid > 0x7fffffff / kBlock || (p.parts > 1 && join > 0x7fffffff / kBlock)) return hipErrorInvalidConfiguration;
     const float sl2 = (scale > 0.0f ? scale : 1.0f / sqrtf(static_cast<float>(kD))) * 1.4426950408889634f;
     float* po = static_cast<float*>(ws);
@@ -487,7 +569,9 @@ hipError_t launch_chunk_attn(const Dims& d, const CacheView& c, const ChunkView&
                  : (c.table ? launch_kernel(chunk_rows_kernel<DTV, ODTV, true>, static_cast<int>(grid), kBlock, s, a)       \
                             : launch_kernel(chunk_rows_kernel<DTV, ODTV, false>, static_cast<int>(grid), kBlock, s, a));    \
     if (e == hipSuccess && p.parts > 1)                                                                                     \
-        e = launch_kernel(chunk_join_kernel<ODTV>, static_cast<int>(join), kBlock, s, a, p.tile_rows)
+        e = p.tokens           ? launch_kernel(join_tokens_kernel<ODTV>, static_cast<int>(join), kBlock, s, a)              \
+            : join_splits(p)   ? launch_kernel(join_rows_kernel<ODTV, true>, static_cast<int>(join), kBlock, s, a, blocks)  \
+                               : launch_kernel(join_rows_kernel<ODTV, false>, static_cast<int>(join), kBlock, s, a, blocks)
     if (d.kv_dtype == kBF16) {
         if (d.out_dtype == kF32) {
             SIK_CHUNK(kBF16, kF32);

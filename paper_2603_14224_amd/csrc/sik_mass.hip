@@ -150,7 +150,7 @@ hipError_t launch_mass(const Dims& d, const CacheView& c, const ChunkView& ch, c
                        const float* lse, int n_obs, const float* before, float* mass, hipStream_t s) {
     const int blocks = (d.Lmax + 127) / 128;
     const int64_t grid = static_cast<int64_t>(blocks) * d.units();
-    if (grid > 0x7fffffff / kBlock) return hipErrorInvalidConfiguration;
+    if (grid > 0x7fffffff / kBlock || static_cast<int64_t>(ch.n) * d.R > 0x7fffffff - kMassStage) return hipErrorInvalidConfiguration;
     const float sl2 = (scale > 0.0f ? scale : 1.0f / sqrtf(static_cast<float>(kD))) * 1.4426950408889634f;
     const MassArgs a{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(K), lse, c, ch, d.Hq, d.R, blocks, n_obs,
                      sl2, before, mass};
