@@ -509,11 +509,19 @@ __global__ __launch_bounds__(kBlock) void join_rows_kernel(const ChunkAttn a, in
     if (a.lse && x == 0) a.lse[at] = log_sum(M, l);
 }
 
-// Form and split of a call.  The `rows` form runs two workgroups to a compute unit, as does the `tokens` form.
+// Form and split of a call.  Both forms run two workgroups to a compute unit, kSlots at a time.
+constexpr int kSlots = 512, kMaxGroups = 3 * kSlots;
 struct ChunkPlan {
     bool tokens;
     int tiles, parts, tile_rows;
 };
+// At least 256 tokens to a part; of short caches in the `tokens` form 128, a step of its four wavefronts, up to 32 parts (one
+// token on 500 to 4000 tokens of 8 KV heads 9.3 to 9.9 us against 10.5 to 11.1; on 8000 63 parts take 12.9, 32 take 11.7).
+static int most_parts(const Dims& d, bool tokens) {
+    int most = (d.Lmax + 255) / 256;
+    if (tokens && most < 32) most = (d.Lmax + 127) / 128 < 32 ? (d.Lmax + 127) / 128 : 32;
+    return most < kMaxParts ? most : kMaxParts;
+}
 static ChunkPlan chunk_plan(const Dims& d, int n) {
     ChunkPlan p;
     const int64_t rows = static_cast<int64_t>(n) * d.R;
@@ -521,11 +529,34 @@ static ChunkPlan chunk_plan(const Dims& d, int n) {
     p.tile_rows = p.tokens ? kTokensTile : kRowsTile;
     p.tiles = static_cast<int>((rows + p.tile_rows - 1) / p.tile_rows);
     const int64_t groups = static_cast<int64_t>(d.units()) * p.tiles;
-    int64_t parts = (512 + groups - 1) / groups;
-    const int64_t most = (d.Lmax + 511) / 512;  // at least 512 tokens to a part
-    if (parts > most) parts = most;
-    if (parts > kMaxParts) parts = kMaxParts;
-    p.parts = static_cast<int>(parts < 1 ? 1 : parts);
+    p.parts = 1;
+    const int most = most_parts(d, p.tokens);
+    if (p.tokens) {
+        // memory-bound: one round of workgroups (one token on 32767 tokens of 8 KV heads: 28 us in 64 parts, 31 in 96; on 8000
+        // 11.7 us in 32 parts, 44 in two)
+        const int64_t by_slots = kSlots / groups;
+        p.parts = static_cast<int>(by_slots < 1 ? 1 : by_slots < most ? by_slots : most);
+        return p;
+    }
+    // Cost of a split in tiles of 64 tokens, a part's state and its join counted as six (a lone part's start as two): rounds
+    // of workgroups, as if all sequences were as long as the cache; in a batch, where they seldom are, plus the same with
+    // lengths spread (two thirds on average, half of the last round idle).  333 tokens behind 9000 of 6 x 8 KV heads with
+    // 5:1 heads: two parts 464 us against 516 of one, with unequal lengths 247 against 274; 100 behind 16000 of 8 x 8 with
+    // 8:1, unequal: 270 against 436; 64 behind 2000 of 16 x 8 with 4:1: two parts 56, four 66.
+    const float T = static_cast<float>((d.Lmax + 63) / 64);
+    float best = 0.0f;
+    for (int k = 1; k <= most && (k == 1 || groups * k <= kMaxGroups); ++k) {
+        const float part = T / k, extra = k == 1 ? 2.0f : 6.0f, g = static_cast<float>(groups);
+        float cost = static_cast<float>((groups * k + kSlots - 1) / kSlots) * (part + extra);
+        if (d.B > 1) {
+            const float spread = g * (0.65f * T + k * extra) / kSlots + 0.5f * (part + extra);
+            cost += spread > part + extra ? spread : part + extra;
+        }
+        if (k == 1 || cost < best) {
+            best = cost;
+            p.parts = k;
+        }
+    }
     return p;
 }
 
@@ -541,14 +572,11 @@ static size_t plan_rows(const Dims& d, const ChunkPlan& p) {
 }
 
 size_t chunk_attn_bytes(const Dims& d, int n) {
-    // the most that any chunk of up to n tokens needs: fewer row tiles have more parts
-    size_t most = 0;
-    for (int64_t m = 1; m <= n; m = m < 1024 ? m + 1 : m * 2) {
-        const size_t r = plan_rows(d, chunk_plan(d, static_cast<int>(m)));
-        if (r > most) most = r;
-    }
-    const size_t r = plan_rows(d, chunk_plan(d, n));
-    return (r > most ? r : most) * (kD + 2) * 4;
+    // what any chunk of up to n tokens needs, whatever its plan: no split has more than kMaxGroups workgroups
+    const int64_t parts = most_parts(d, true), tiles = (static_cast<int64_t>(n) * d.R + kRowsTile - 1) / kRowsTile;
+    auto bound = [&](int64_t groups, int64_t cap) { return groups > cap / parts ? cap : groups * parts; };
+    const int64_t r = bound(d.units() * tiles, kMaxGroups) * kRowsTile, t = bound(d.units(), kSlots) * kTokensTile;
+    return parts == 1 ? 0 : static_cast<size_t>(r > t ? r : t) * (kD + 2) * 4;
 }
 
 hipError_t launch_chunk_attn(const Dims& d, const CacheView& c, const ChunkView& ch, const void* q, const void* K,
