@@ -192,10 +192,11 @@ __global__ __launch_bounds__(kBlock, 2) void chunk_rows_kernel(const ChunkAttn a
     init_rows(st);
 
     const RowOffsets ko = row_offsets<true>(lane, 15), vo = row_offsets<false>(lane, 15);
+    GroupRows<PAGED> at(a.cv, b, h);
     auto issue = [&](int tile, int buf) {
         int g = tile * kTile + 16 * wv;
         if (g >= end) g = (end - 1) & ~15;
-        const int64_t row = cache_row(a.cv, b, h, g);
+        const int64_t row = at.row(uniform(g));
         const uint16_t *kb = group_row(a.K, row), *vb = group_row(a.V, row);
         if constexpr (PAGED) {
             if (lane == 0) s_mapped[buf][wv] = kb != nullptr;
@@ -210,6 +211,7 @@ __global__ __launch_bounds__(kBlock, 2) void chunk_rows_kernel(const ChunkAttn a
         }
     };
     if (t0 < t1) issue(t0, 0);
+    arrived(qf);
     for (int tile = t0; tile < t1; ++tile) {
         const int buf = (tile - t0) & 1;
         dma_wait<0>();
@@ -287,6 +289,7 @@ __global__ __launch_bounds__(kBlock, 2) void chunk_tokens_kernel(const ChunkAttn
     char* values = keys + kSide;
     const RowOffsets ko = row_offsets<true>(lane, 15), vo = row_offsets<false>(lane, 15);
     uint32_t mapped = 3u;
+    GroupRows<PAGED> at(a.cv, b, h);
     // the two 16-token groups of one of this wavefront's tiles, keys and values one after the other
     auto issue = [&](const uint16_t* x, int tile, bool is_key) {
         uint32_t got = 0;
@@ -294,7 +297,7 @@ __global__ __launch_bounds__(kBlock, 2) void chunk_tokens_kernel(const ChunkAttn
         for (int g2 = 0; g2 < 2; ++g2) {
             int g = tile * kTile + 16 * g2;
             if (g >= end) g = (end - 1) & ~15;
-            const uint16_t* base = group_row(x, cache_row(a.cv, b, h, g));
+            const uint16_t* base = group_row(x, at.row(uniform(g)));
             got |= (base != nullptr) << g2;
             const int last = min(end - 1 - g, 15);
             RowOffsets r = is_key ? ko : vo;
@@ -310,6 +313,7 @@ __global__ __launch_bounds__(kBlock, 2) void chunk_tokens_kernel(const ChunkAttn
         mapped = issue(a.K, tile, true);
         issue(a.V, tile, false);
     }
+    arrived(qf);
     for (; tile < stop; tile += 4) {
         const bool more = tile + 4 < stop;
         dma_wait<8>();

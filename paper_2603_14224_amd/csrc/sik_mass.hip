@@ -99,6 +99,7 @@ __global__ __launch_bounds__(kBlock, 4) void mass_kernel(const MassArgs a) {
 #pragma unroll
     for (int i = 0; i < kMassBuffers - 1; ++i)
         if (i < tiles) load(i);
+    arrived(kf);
     for (int tile = 0; tile < tiles; ++tile) {
         const int row0 = (tile * kMassRows) % kMassStage;
         if (row0 == 0) {

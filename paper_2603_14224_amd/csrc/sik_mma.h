@@ -71,6 +71,13 @@ __device__ __forceinline__ void dma_wait() {
 __device__ __forceinline__ void lds_reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void barrier_only() { asm volatile("s_barrier" ::: "memory"); }
 
+// Fragments that were loaded into registers have arrived.  Without this the compiler would wait for them where a loop first
+// uses them, in every pass, and with them for the loads that the loop keeps on their way.
+__device__ __forceinline__ void arrived(u32x4 (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(f[i]));
+}
+
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 template <class T>
 __device__ __forceinline__ T* uniform(T* p) {
@@ -79,6 +86,33 @@ __device__ __forceinline__ T* uniform(T* p) {
     const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(a >> 32));
     return reinterpret_cast<T*>(static_cast<uint64_t>(hi) << 32 | lo);
 }
+
+// Rows of the 16-token groups of one sequence and head, a group at a time (uniform over the wavefront).  Of a page table the
+// wavefront holds 64 entries, one per lane, so that a group costs a register read and the table a load every 64 pages: a load
+// per group would wait for all the rows that are on their way.
+template <bool PAGED>
+struct GroupRows {
+    const CacheView& c;
+    int64_t first;  // contiguous: row of token 0
+    const int32_t* table;
+    int h, window = -64, held = 0;
+    __device__ __forceinline__ GroupRows(const CacheView& c_, int b, int h_) : c(c_), h(h_) {
+        first = (static_cast<int64_t>(b) * c.Hkv + h) * c.Lmax;
+        if constexpr (PAGED) table = c.table + static_cast<int64_t>(b) * c.per_seq;
+    }
+    // row of token j, -1 without a page
+    __device__ __forceinline__ int64_t row(int j) {
+        if constexpr (!PAGED) return first + j;
+        const int p = j >> c.shift;
+        if (p < window || p >= window + 64) {
+            window = p;
+            held = table[min(p + static_cast<int>(threadIdx.x & 63), c.per_seq - 1)];
+        }
+        const int page = __builtin_amdgcn_readlane(held, p - window);
+        if (static_cast<uint32_t>(page) >= static_cast<uint32_t>(c.n_pages)) return -1;
+        return ((static_cast<int64_t>(page) * c.Hkv + h) << c.shift) + (j & ((1 << c.shift) - 1));
+    }
+};
 
 // What a lane reads when its wavefront loads 16 rows of 256 B in four instructions: row 4 i + l / 16, the piece that the
 // swizzle puts in place l % 16.
