@@ -73,8 +73,9 @@ __device__ __forceinline__ void mask_logits(f32x16 (&s)[NK], int lane, int last,
         }
 }
 
-template <int DT, int NK, bool PREC>
-__device__ __forceinline__ void tile_update(RowState& st, const f32x16 (&s)[NK], const char* values, int lane, float c) {
+// Largest logit of a tile, in powers of two.
+template <int NK>
+__device__ __forceinline__ float tile_top(const f32x16 (&s)[NK], float c) {
     float top = s[0][0];
 #pragma unroll
     for (int t = 0; t < NK; ++t)
@@ -82,17 +83,26 @@ __device__ __forceinline__ void tile_update(RowState& st, const f32x16 (&s)[NK],
         for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
     float lo, hi;
     both_halves(top, lo, hi);
-    top = fmaxf(lo, hi) * c;
-    if (__any(top > st.m + kSlack)) {
-        const float m = fmaxf(st.m, top), f = fast_exp2(st.m - m);
-        st.m = m;
-        st.l *= f;
+    return fmaxf(lo, hi) * c;
+}
+
+__device__ __forceinline__ void rescale(RowState& st, float top) {
+    const float m = fmaxf(st.m, top), f = fast_exp2(st.m - m);
+    st.m = m;
+    st.l *= f;
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
+    for (int b = 0; b < 4; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) st.o[b][i] *= f;
-    }
+        for (int i = 0; i < 16; ++i) st.o[b][i] *= f;
+}
+
+// A tile's weights as operands, a group of 16 tokens in each; PREC: and what their rounding dropped.
+template <int NK, bool PREC>
+struct Weights {
     u32x4 w[2 * NK], rest[PREC ? 2 * NK : 1];
+};
+template <int DT, int NK, bool PREC>
+__device__ __forceinline__ void tile_weights(RowState& st, const f32x16 (&s)[NK], float c, Weights<NK, PREC>& x) {
     float sum = 0.0f;
 #pragma unroll
     for (int t = 0; t < NK; ++t)
@@ -102,18 +112,22 @@ __device__ __forceinline__ void tile_update(RowState& st, const f32x16 (&s)[NK],
             sum += a;
             sum += b;
             const uint32_t p = pack16<DT>(a, b);
-            w[2 * t + i / 8][(i % 8) / 2] = p;
+            x.w[2 * t + i / 8][(i % 8) / 2] = p;
             if constexpr (PREC)
-                rest[2 * t + i / 8][(i % 8) / 2] = pack16<DT>(a - widen16<DT>(p & 0xffffu), b - widen16<DT>(p >> 16));
+                x.rest[2 * t + i / 8][(i % 8) / 2] = pack16<DT>(a - widen16<DT>(p & 0xffffu), b - widen16<DT>(p >> 16));
         }
     st.l += sum;
+}
+
+template <int DT, int NK, bool PREC>
+__device__ __forceinline__ void tile_values(RowState& st, const Weights<NK, PREC>& x, const char* values, int lane) {
 #pragma unroll
     for (int g = 0; g < 2 * NK; ++g)
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             const u32x4 v = value_fragment(values + g * 16 * 256, lane, b);
-            st.o[b] = mma32<DT>(v, w[g], st.o[b]);
-            if constexpr (PREC) st.o[b] = mma32<DT>(v, rest[g], st.o[b]);
+            st.o[b] = mma32<DT>(v, x.w[g], st.o[b]);
+            if constexpr (PREC) st.o[b] = mma32<DT>(v, x.rest[g], st.o[b]);
         }
 }
 
@@ -193,42 +207,81 @@ __global__ __launch_bounds__(kBlock, 2) void chunk_rows_kernel(const ChunkAttn a
 
     const RowOffsets ko = row_offsets<true>(lane, 15), vo = row_offsets<false>(lane, 15);
     GroupRows<PAGED> at(a.cv, b, h);
-    auto issue = [&](int tile, int buf) {
+    auto issue = [&](const uint16_t* x, int tile, bool is_key) {
         int g = tile * kTile + 16 * wv;
         if (g >= end) g = (end - 1) & ~15;
-        const int64_t row = at.row(uniform(g));
-        const uint16_t *kb = group_row(a.K, row), *vb = group_row(a.V, row);
+        const int buf = (tile - t0) & 1, last = end - 1 - g;
+        const uint16_t* base = group_row(x, at.row(uniform(g)));
         if constexpr (PAGED) {
-            if (lane == 0) s_mapped[buf][wv] = kb != nullptr;
+            if (is_key && lane == 0) s_mapped[buf][wv] = base != nullptr;
         }
-        const uint32_t to = buf * kBuf + wv * 16 * 256;
-        if (end - 1 - g >= 15) {
-            load_rows16(kb, ko, to, lds, lane);
-            load_rows16(vb, vo, to + kSide, lds, lane);
-        } else {  // the group holds the last token
-            load_rows16(kb, row_offsets<true>(lane, end - 1 - g), to, lds, lane);
-            load_rows16(vb, row_offsets<false>(lane, end - 1 - g), to + kSide, lds, lane);
-        }
+        const uint32_t to = buf * kBuf + (is_key ? 0 : kSide) + wv * 16 * 256;
+        if (last >= 15)
+            load_rows16(base, is_key ? ko : vo, to, lds, lane);
+        else  // the group holds the last token
+            load_rows16(base, is_key ? row_offsets<true>(lane, last) : row_offsets<false>(lane, last), to, lds, lane);
     };
-    if (t0 < t1) issue(t0, 0);
-    arrived(qf);
-    for (int tile = t0; tile < t1; ++tile) {
-        const int buf = (tile - t0) & 1;
+    // Tile by tile, the logits of the next one are computed beside the weights of this one: the matrix units have work while
+    // the exponentials run.  So keys are loaded two tiles ahead, values one.
+    const int tw = w0 < rows ? min(t1, (past + last_t) / kTile + 1) : t0;  // tiles beyond tw: masked for all of the wavefront
+    auto arrive = [&](int tile) {
         dma_wait<0>();
         lds_reads_done();
         barrier_only();
-        if (tile + 1 < t1) issue(tile + 1, buf ^ 1);
-        if (w0 >= rows || tile * kTile > past + last_t) continue;
-        const char* keys = lds + buf * kBuf;
-        f32x16 s[2];
-        tile_logits<DT, 2>(keys, lane, qf, s);
+        if (tile + 2 < t1) issue(a.K, tile + 2, true);
+        if (tile + 1 < t1) issue(a.V, tile + 1, false);
+    };
+    auto side = [&](int tile) { return lds + ((tile - t0) & 1) * kBuf; };
+    float top = kNegBig;
+    auto masked_top = [&](f32x16(&s)[2], int tile) {
         uint32_t mapped = 15u;
-        if constexpr (PAGED)
-            mapped = uniform(s_mapped[buf][0] | s_mapped[buf][1] << 1 | s_mapped[buf][2] << 2 | s_mapped[buf][3] << 3);
+        if constexpr (PAGED) {
+            const int* x = s_mapped[(tile - t0) & 1];
+            mapped = uniform(x[0] | x[1] << 1 | x[2] << 2 | x[3] << 3);
+        }
         if (tile * kTile + kTile - 1 > past + first_t || mapped != 15u)
             mask_logits<2>(s, lane, past + t - tile * kTile, mapped);
-        tile_update<DT, 2, ODT == kF32>(st, s, keys + kSide, lane, a.scale_log2e);
+        top = tile_top<2>(s, a.scale_log2e);
+        return __any(top > st.m + kSlack) != 0;
+    };
+    // one tile, whose logits are s; the next one's to n; true: the maximum has to move before they can be used
+    auto step = [&](const f32x16(&s)[2], f32x16(&n)[2], int tile) {
+        arrive(tile);
+        Weights<2, ODT == kF32> w;
+        tile_weights<DT, 2>(st, s, a.scale_log2e, w);
+        tile_logits<DT, 2>(side(tile + 1), lane, qf, n);  // (after the last tile of what lies there, and not used)
+        tile_values<DT, 2>(st, w, side(tile) + kSide, lane);
+        return tile + 1 < tw && masked_top(n, tile + 1);
+    };
+    f32x16 s[2], n[2];
+    if (t0 < t1) {
+        issue(a.K, t0, true);
+        arrived(qf);
+        dma_wait<0>();
+        lds_reads_done();
+        barrier_only();
+        issue(a.V, t0, false);
+        if (t0 + 1 < t1) issue(a.K, t0 + 1, true);
     }
+    int tile = t0;
+    bool moved = false;
+    if (tile < tw) {
+        tile_logits<DT, 2>(side(tile), lane, qf, s);
+        moved = masked_top(s, tile);
+    }
+    while (tile < tw) {
+        if (moved) rescale(st, top);
+        // (left only where the maximum moves: the output registers stay where they are while it does not)
+        for (moved = false; tile < tw && !moved;) {
+            moved = step(s, n, tile++);
+            if (moved || tile >= tw) {
+                s[0] = n[0], s[1] = n[1];
+                break;
+            }
+            moved = step(n, s, tile++);
+        }
+    }
+    for (; tile < t1; ++tile) arrive(tile);
     float lo, hi;
     both_halves(st.l, lo, hi);
     const float l = lo + hi;
@@ -329,7 +382,11 @@ __global__ __launch_bounds__(kBlock, 2) void chunk_tokens_kernel(const ChunkAttn
             dma_wait<8>();
         else
             dma_wait<0>();
-        tile_update<DT, 1, ODT == kF32>(st, s, values, lane, a.scale_log2e);
+        const float top = tile_top<1>(s, a.scale_log2e);
+        if (__any(top > st.m + kSlack)) rescale(st, top);
+        Weights<1, ODT == kF32> w;
+        tile_weights<DT, 1>(st, s, a.scale_log2e, w);
+        tile_values<DT, 1>(st, w, values, lane);
         lds_reads_done();
         if (more) issue(a.V, tile + 4, false);
         mapped = next;
