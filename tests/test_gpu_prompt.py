@@ -165,6 +165,8 @@ CHUNK = [
     (1, 4, 4, 40, [9000], None, 0, BF, BF),
     (1, 1, 100, 3, [257], None, 0, BF, BF),
     (2, 1, 3, 7, [5000, 12], None, 1024, FP, torch.float32),
+    (1, 8, 32, 64, [1500], None, 0, BF, BF),
+    (3, 2, 8, 40, [4000, 0, 130], [40, 40, 3], 16, FP, FP),
 ]
 
 
@@ -293,6 +295,9 @@ MASS = [
     (1, 1, 7, 200, [63], None, 0, FP, 33, False),
     (1, 2, 16, 300, [0], None, 64, BF, 300, False),
     (2, 1, 100, 5, [700, 2], None, 0, FP, 3, True),
+    (2, 8, 32, 200, [1200, 100], [200, 77], 0, BF, 200, True),   # many tokens: a wavefront owns 32, sums in two stages
+    (4, 8, 40, 150, [700, 64, 0, 699], [150, 1, 150, 149], 16, FP, 150, False),
+    (1, 1, 3, 700, [5], None, 0, BF, 700, True),                 # few tokens, many queries
 ]
 
 
@@ -342,6 +347,9 @@ EVICT = [
     (1, 2, [70000], 2048, 4, 1, 0, BF, "steps"),
     (1, 1, [140001], 5000, 0, 7, 0, FP, "plain"),
     (1, 3, [9000], 500, 0, 0, 64, FP, "signs"),
+    (1, 1, [600001], 3000, 2, 5, 0, BF, "plain"),   # chunks longer than what a workgroup holds in registers
+    (1, 1, [600001], 3000, 2, 5, 0, BF, "equal"),   # every token in the cut's bin
+    (2, 1, [20000, 9000], 9500, 9000, 500, 0, BF, "plain"),  # nothing to choose
 ]
 
 

@@ -10,7 +10,7 @@ def kernels():
 
 
 @pytest.mark.parametrize("part", ["rope_kernel", "chunk_rows_kernel", "chunk_tokens_kernel", "join_tokens_kernel",
-                                  "join_rows_kernel", "mass_kernel", "evict_select_kernel", "evict_count_kernel",
+                                  "join_rows_kernel", "mass_kernel", "mass_split_kernel", "evict_select_kernel", "evict_count_kernel",
                                   "evict_collect_kernel", "evict_place_kernel", "evict_rows_kernel"])
 def test_no_scratch_memory(kernels, part):
     some = {n: k for n, k in kernels.items() if part in n}
