@@ -1,9 +1,9 @@
 // Eviction by accumulated attention weight: the tokens that stay, in ascending order, and the cache cut down to them.
 //
 // The cut is found by a radix selection on order-preserving keys of 32 bits, in digits of 11, 11 and 10 bits; what stays is
-// placed from bit counts, in token order, so the list needs no sort and no atomics decide an order.  Short caches: one
-// workgroup per (sequence, KV head) holds the weights in its registers.  Longer ones in three launches of many workgroups, a
-// chunk of tokens each: `count` (first digit of every chunk), `collect` (every workgroup adds the chunks' counts up, finds the
+// placed from bit counts, in token order, so the list needs no sort and no atomics decide an order.  Short caches, and longer
+// ones in large batches: one workgroup per (sequence, KV head) holds the weights in its registers.  Else three launches of many
+// workgroups, a chunk of tokens each: `count` (first digit of every chunk), `collect` (every workgroup adds the chunks' counts up, finds the
 // cut's bin and writes its tokens of that bin, a few per cent, behind those of the chunks before), `place` (the other two
 // digits from those tokens alone, then the chunk's part of the list).
 #include "sik_chunk.h"
@@ -14,7 +14,7 @@ constexpr int kEvictBlock = 1024;
 constexpr int kDigitBins = 2048;   // of the first two digits; the last one has 1024
 constexpr int kChunkTokens = 8192; // tokens of a chunk, more where there would be more than kEvictChunks of them
 constexpr int kEvictChunks = 64;
-constexpr int kEvictDirect = 8192; // caches up to this length take one workgroup per row (8 weights per thread)
+constexpr int kEvictStep = 4096;   // tokens of a workgroup at four weights per thread
 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));  // rows start at any multiple of 4 bytes
 
@@ -123,9 +123,11 @@ __device__ __forceinline__ void before_wave(uint32_t a, uint32_t b, uint32_t (*t
     }
 }
 
-// ---- short caches: one workgroup per row ------------------------------------------------------------------------------
+// ---- one workgroup per row ------------------------------------------------------------------------------
+// NV: steps of 256 tokens that a wavefront holds, so kEvictStep NV tokens to a row at most.
+template <int NV>
 __global__ __launch_bounds__(kEvictBlock) void evict_select_kernel(EvictArgs a, int Hkv, int Lmax) {
-    constexpr int kWaves = kEvictBlock / kWave, NV = kEvictDirect / (4 * kEvictBlock);
+    constexpr int kWaves = kEvictBlock / kWave;
     __shared__ uint32_t hist[kDigitBins];
     __shared__ uint32_t totals[kWaves], found[2], s_tot[kWaves][2];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -162,26 +164,31 @@ __global__ __launch_bounds__(kEvictBlock) void evict_select_kernel(EvictArgs a, 
         find_digit<kEvictBlock>(c, d, need, totals, found);
         cut = cut << (digit == 2 ? 10 : 11) | d;
     }
-    bool sure[NV][4], equal[NV][4];
+    auto sure_of = [&](int j, float x) { return j < r.L && (!r.inner(j) || (r.need > 0 && float_to_key(x) > cut)); };
+    auto equal_of = [&](int j, float x) { return r.need > 0 && r.inner(j) && float_to_key(x) == cut; };
     uint32_t ns = 0, ne = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int j = at + 256 * i + e;
-            const uint32_t key = float_to_key(v[i][e]);
-            sure[i][e] = j < r.L && (!r.inner(j) || (r.need > 0 && key > cut));
-            equal[i][e] = r.need > 0 && r.inner(j) && key == cut;
-            ns += __popcll(__ballot(sure[i][e]));
-            ne += __popcll(__ballot(equal[i][e]));
+            ns += __popcll(__ballot(sure_of(at + 256 * i + e, v[i][e])));
+            ne += __popcll(__ballot(equal_of(at + 256 * i + e, v[i][e])));
         }
     uint32_t ps = 0, pe = 0;
     before_wave<kWaves>(ns, ne, s_tot, ps, pe);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) place4(keep, at + 256 * i, sure[i], equal[i], need, ps, pe);
+    for (int i = 0; i < NV; ++i) {
+        bool sure[4], equal[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            sure[e] = sure_of(at + 256 * i + e, v[i][e]);
+            equal[e] = equal_of(at + 256 * i + e, v[i][e]);
+        }
+        place4(keep, at + 256 * i, sure, equal, need, ps, pe);
+    }
 }
 
-// ---- long caches: a workgroup per chunk of `per` tokens -----------------------------------------------------------------
+// ---- a workgroup per chunk of `per` tokens -----------------------------------------------------------------
 struct EvictScratch {
     uint32_t* counts;  // [unit][chunk][kDigitBins]  first digits
     uint32_t* list;    // [unit][list_len]           keys of the tokens in the cut's bin, in token order
@@ -441,12 +448,19 @@ __global__ __launch_bounds__(kBlock) void evict_rows_kernel(EvictArgs a, CacheVi
     }
 }
 
+// One workgroup per row (us for 1 / 128 / 256 rows against the three launches): 16370 tokens 20.7 / 21.9 / 22.9 against 21.1 /
+// 24.0 / 39.6; beyond 16384 only where the rows fill half of the chip: 20000 tokens 25 / 26.0 / 27.1 against 21.4 / 38.5 / 54.6,
+// 32000 38.5 / 40.2 / 42.2 against 21.5 / 41.4 / 73.7.
+static bool evict_direct(const Dims& d) {
+    return d.Lmax <= 4 * kEvictStep || (d.Lmax <= 8 * kEvictStep && d.units() >= 128);
+}
+
 static EvictScratch evict_plan(const Dims& d, void* ws, size_t* bytes) {
     EvictScratch w{};
     w.per = kChunkTokens;
     const int least = (d.Lmax + kEvictChunks - 1) / kEvictChunks;
     if (least > w.per) w.per = (least + 4095) / 4096 * 4096;
-    w.chunks = d.Lmax <= kEvictDirect ? 0 : (d.Lmax + w.per - 1) / w.per;
+    w.chunks = evict_direct(d) ? 0 : (d.Lmax + w.per - 1) / w.per;
     w.list_len = d.Lmax;
     const int64_t units = d.units(), rows = units * w.chunks;
     uint32_t* p = static_cast<uint32_t*>(ws);
@@ -475,7 +489,16 @@ hipError_t launch_evict(const Dims& d, const CacheView& c, const EvictArgs& a, v
         return hipErrorInvalidConfiguration;
     hipError_t e;
     if (w.chunks == 0) {
-        e = launch_kernel(evict_select_kernel, d.units(), kEvictBlock, s, a, d.Hkv, d.Lmax);
+        auto select = [&](auto kernel) { return launch_kernel(kernel, d.units(), kEvictBlock, s, a, d.Hkv, d.Lmax); };
+        switch ((d.Lmax + kEvictStep - 1) / kEvictStep) {
+            case 1: e = select(evict_select_kernel<1>); break;
+            case 2: e = select(evict_select_kernel<2>); break;
+            case 3: e = select(evict_select_kernel<3>); break;
+            case 4: e = select(evict_select_kernel<4>); break;
+            case 5: e = select(evict_select_kernel<5>); break;
+            case 6: e = select(evict_select_kernel<6>); break;
+            default: e = select(evict_select_kernel<8>);
+        }
     } else {
         const int grid = static_cast<int>(chunks);
         e = hipSuccess;
