@@ -348,8 +348,8 @@ int sik_decode_step_ex(const sik_layout *layout, const sik_decode_args *args);
  * A chunk is n new tokens per sequence, of which sequence b has n_new[b] (values are clamped to [0, n]); rows of the
  * chunk's tensors at or beyond n_new[b] are neither read nor written.  seq_len[b] (clamped to [0, max_len]) is the number
  * of tokens in the cache BEFORE the chunk; token t of the chunk is cache row seq_len[b] + t, and tokens at or beyond
- * max_len are dropped (not written, and as queries their output rows are left as they were).  No call
- * here changes seq_len: add n_new to it once the chunk went through the layers.
+ * max_len are dropped (not written, and as queries their output rows are left as they were; n_new[b] below is what remains).
+ * No call here changes seq_len: add n_new to it once the chunk went through the layers.
  *
  * Both blocks are host structures that hold device pointers; zero-initialise them and set what applies. */
 typedef struct {
@@ -415,14 +415,15 @@ int sik_chunk_attn(const sik_layout *layout, const sik_chunk *chunk, const void 
  *                 exp(softmax_scale * q[b,t,hq] . K_j - lse[b,t,hq])
  * mass, before [B,Hkv,max_len] float; before = NULL: 0; before = mass adds in place.  Entries beyond the sequence are left
  * as they were; tokens on unmapped pages receive nothing.  lse as written by sik_chunk_attn (a row with -infinity
- * contributes nothing); 1 <= n_obs <= n. */
+ * contributes nothing); 1 <= n_obs <= n.  Sums that are kept over several chunks need zeros for the tokens to come. */
 int sik_attn_mass(const sik_layout *layout, const sik_chunk *chunk, const void *q, const void *K, float softmax_scale,
                   const float *lse, int32_t n_obs, const float *before, float *mass, void *stream);
 
-/* Eviction: per (sequence, KV head) the n_keep tokens that stay, L = seq_len[b] (clamped to [0, max_len]): the first n_sink, the last n_recent and of
- * those between them the n_keep - n_sink - n_recent with the largest mass [B,Hkv,max_len] (equal masses: the smaller
- * index first; no NaN).  With L <= n_keep every token stays.  keep [B,Hkv,n_keep] int32 receives them in ascending order,
- * -1 beyond; new_len [B] (may be NULL) min(L, n_keep).  n_sink, n_recent >= 0, n_sink + n_recent <= n_keep <= max_len.
+/* Eviction: per (sequence, KV head) the n_keep tokens that stay, L = seq_len[b] (clamped to [0, max_len]): the first
+ * n_sink, the last n_recent and of those between them the n_keep - n_sink - n_recent with the largest mass
+ * [B,Hkv,max_len] (equal masses: the smaller index first; no NaN among the L; what lies behind them is not used).  With
+ * L <= n_keep every token stays.  keep [B,Hkv,n_keep] int32 receives them in ascending order, -1 beyond; new_len [B] (may
+ * be NULL) min(L, n_keep).  n_sink, n_recent >= 0, n_sink + n_recent <= n_keep <= max_len.
  * With K_out and V_out (both or neither) the cache is cut down as well: rows keep[b,h,i] of K, V (contiguous, or paged by
  * `pages`; a token on an unmapped page gives a zero row) become rows i of K_out, V_out [B,Hkv,out_len,D], out_len >=
  * n_keep; rows beyond new_len are left as they were.  mass_out [B,Hkv,out_len] (may be NULL) receives their masses.  The

@@ -130,7 +130,8 @@ int sik_evict(const sik_layout* layout, const sik_evict_args* a) {
     if (!a->K_out != !a->V_out) return SIK_ERR_NULL;
     if (a->K_out) {
         if (!a->K || !a->V) return SIK_ERR_NULL;
-        if (a->K_out == a->K || a->V_out == a->V || a->K_out == a->V_out || a->K_out == a->V || a->V_out == a->K) return SIK_ERR_FLAGS;
+        if (a->K_out == a->K || a->V_out == a->V || a->K_out == a->V_out || a->K_out == a->V || a->V_out == a->K)
+            return SIK_ERR_FLAGS;
         if (misaligned(a->K) || misaligned(a->V) || misaligned(a->K_out) || misaligned(a->V_out)) return SIK_ERR_ALIGN;
     }
     if (a->mass_out == a->mass) return SIK_ERR_FLAGS;

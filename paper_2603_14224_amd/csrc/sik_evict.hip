@@ -3,9 +3,12 @@
 // The cut is found by a radix selection on order-preserving keys of 32 bits, in digits of 11, 11 and 10 bits; what stays is
 // placed from bit counts, in token order, so the list needs no sort and no atomics decide an order.  Short caches, and longer
 // ones in large batches: one workgroup per (sequence, KV head) holds the weights in its registers.  Else three launches of many
-// workgroups, a chunk of tokens each: `count` (first digit of every chunk), `collect` (every workgroup adds the chunks' counts up, finds the
-// cut's bin and writes its tokens of that bin, a few per cent, behind those of the chunks before), `place` (the other two
-// digits from those tokens alone, then the chunk's part of the list).
+// workgroups, a chunk of tokens each: `count` (first digit of every chunk), `collect` (every workgroup adds the chunks' counts
+// up, finds the cut's bin and writes its tokens of that bin, a few per cent, behind those of the chunks before), `place` (the
+// other two digits from those tokens alone, then the chunk's part of the list).
+//
+// Bounds: the list, chains of memory, counting and barriers (32 rows of 65536 weights in 34 us, of which 5, 6 and 8 inside the
+// launches; 256 rows of 16370 in 23); the rows, memory (2048 rows of K and V for each of 256, 537 MB: 92 us, 5.9 TB/s).
 #include "sik_chunk.h"
 
 namespace sik {
@@ -83,7 +86,8 @@ __device__ __forceinline__ void find_digit(const uint32_t (&c)[NB], uint32_t& di
     need = found[1];
 }
 
-// Places what stays of four consecutive tokens per lane (from i): `sure` ones, and of those `equal` to the cut the first `need`.
+// Places what stays of four consecutive tokens per lane (from i): `sure` ones, and of those `equal` to the cut the first
+// `need`.
 // ps, pe: sure and equal tokens before this wavefront's step, advanced by it.
 __device__ __forceinline__ void place4(int32_t* keep, int i, const bool (&sure)[4], const bool (&equal)[4], uint32_t need,
                                        uint32_t& ps, uint32_t& pe) {
@@ -449,8 +453,8 @@ __global__ __launch_bounds__(kBlock) void evict_rows_kernel(EvictArgs a, CacheVi
 }
 
 // One workgroup per row (us for 1 / 128 / 256 rows against the three launches): 16370 tokens 20.7 / 21.9 / 22.9 against 21.1 /
-// 24.0 / 39.6; beyond 16384 only where the rows fill half of the chip: 20000 tokens 25 / 26.0 / 27.1 against 21.4 / 38.5 / 54.6,
-// 32000 38.5 / 40.2 / 42.2 against 21.5 / 41.4 / 73.7.
+// 24.0 / 39.6; beyond 16384 only where the rows fill half of the chip: 20000 tokens 25 / 26.0 / 27.1 against 21.4 / 38.5 /
+// 54.6, 32000 38.5 / 40.2 / 42.2 against 21.5 / 41.4 / 73.7.
 static bool evict_direct(const Dims& d) {
     return d.Lmax <= 4 * kEvictStep || (d.Lmax <= 8 * kEvictStep && d.units() >= 128);
 }

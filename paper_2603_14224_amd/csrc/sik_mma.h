@@ -58,7 +58,14 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p) {
 }
 
 // 64 x 16 B from base + off (bytes, per lane) to LDS [to, to + 1 KB).  Written in assembly because the compiler would wait
-// for it before every LDS read that follows; dma_wait is the wait.
+// for it before every LDS read that follows; dma_wait is the wait.  A base may come from a vector instruction
+// (readfirstlane), and a memory instruction may read such a scalar register only five states later: dma_base sees to that,
+// which the compiler does not do for assembly.
+template <class T>
+__device__ __forceinline__ T* dma_base(T* base) {
+    asm volatile("s_nop 4" : "+s"(base));
+    return base;
+}
 __device__ __forceinline__ void dma_16(const void* base, uint32_t off, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
 }
@@ -139,6 +146,7 @@ __device__ __forceinline__ void load_rows16(const uint16_t* base, const RowOffse
         return;
     }
     const uint32_t at = lds_offset(lds) + to;
+    base = dma_base(base);
 #pragma unroll
     for (int i = 0; i < 4; ++i) dma_16(base, r.off[i], uniform(static_cast<int>(at + i * 1024)));
 }

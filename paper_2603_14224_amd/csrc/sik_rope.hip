@@ -4,19 +4,26 @@
 // heads, then its key heads, then (into a cache) its value heads, which are copied.  A lane needs the channels that its own
 // are paired with: the same 16 bytes of another lane, loaded a second time (from the first-level cache) rather than
 // exchanged.  The angles of a token are the same for all its heads: a wavefront computes them once, in front of its steps.
+//
+// Bound by memory: 8192 tokens of 40 rows rotated and 8 copied, 201 MB, in 41 us where the outputs stay in the Infinity Cache
+// and in 53 to 57 where they do not (3.5 TB/s; a copy reaches 4.7).  Requests one step ahead (76 us), two steps at a time
+// (62), the partners exchanged between lanes (70) and streaming stores on top of these (66 to 72) were all slower there; one
+// token takes 3.5 us.
 #include "sik_chunk.h"
 
 namespace sik {
 
-// sin and cos of position * freq: the product of 31 and 24 bits is all but exact in 64 bits (exact for
-// positions below 2^29), the whole turns go in 64 bits too (in 32 bits a position of a million would be off by 0.06 rad), what is left of a turn fits 32.
+// sin and cos of position * freq: the product of 31 and 24 bits is all but exact in 64 bits (exact for positions below 2^29),
+// the whole turns go in 64 bits too (in 32 bits a position of a million would be off by 0.06 rad), what is left of a turn
+// fits 32.
 __device__ __forceinline__ void turn(int position, float freq, float& s, float& c) {
     const double rev = static_cast<double>(position) * static_cast<double>(freq) * 0.15915494309189533577;
     sincospif(2.0f * static_cast<float>(rev - rint(rev)), &s, &c);
 }
 
 template <int DT, bool PAIRS>
-__global__ __launch_bounds__(kBlock) void rope_kernel(RopeArgs a, CacheView cv, ChunkView ch, int B, int Hq, int steps, int waves) {
+__global__ __launch_bounds__(kBlock) void rope_kernel(RopeArgs a, CacheView cv, ChunkView ch, int B, int Hq, int steps,
+                                                      int waves) {
     const int lane = threadIdx.x & 63, slot = lane >> 4, p = lane & 15;
     const int w = blockIdx.x * (kBlock / kWave) + (threadIdx.x >> 6);  // wavefront: (sequence, token, part of the heads)
     const int part = w % waves, tok = w / waves;
@@ -106,7 +113,8 @@ hipError_t launch_rope(const Dims& d, const CacheView& c, const ChunkView& ch, c
     const int waves = (groups + steps - 1) / steps;
     const int64_t blocks = (tokens * waves + kBlock / kWave - 1) / (kBlock / kWave);
     if (blocks > 0x7fffffff / kBlock) return hipErrorInvalidConfiguration;
-#define SIK_ROPE(DTV, PV) launch_kernel(rope_kernel<DTV, PV>, static_cast<int>(blocks), kBlock, s, a, c, ch, d.B, d.Hq, steps, waves)
+#define SIK_ROPE(DTV, PV) \
+    launch_kernel(rope_kernel<DTV, PV>, static_cast<int>(blocks), kBlock, s, a, c, ch, d.B, d.Hq, steps, waves)
     if (d.kv_dtype == kBF16) return interleaved ? SIK_ROPE(kBF16, true) : SIK_ROPE(kBF16, false);
     return interleaved ? SIK_ROPE(kF16, true) : SIK_ROPE(kF16, false);
 #undef SIK_ROPE

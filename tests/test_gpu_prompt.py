@@ -391,6 +391,9 @@ def test_evict(B, Hkv, lengths, n_keep, n_sink, n_recent, page, dtype, kind):
     only = torch.full_like(keep, -5)  # the list alone
     sik.sik_evict(lay, mass, ints(lengths), n_keep, only, ws, n_sink=n_sink, n_recent=n_recent)
     assert torch.equal(only, keep)
+    alone = torch.full_like(mo, 7.0)  # and with the masses
+    sik.sik_evict(lay, mass, ints(lengths), n_keep, only, ws, n_sink=n_sink, n_recent=n_recent, mass_out=alone)
+    assert torch.equal(only, keep) and torch.equal(alone, mo)
 
 
 # --------------------------------------------------------------------------------------------- together
