@@ -1,17 +1,20 @@
 // Attention weight that each cached token receives from the last queries of a chunk.
 //
 // A wavefront owns 32 tokens: their keys stay in its registers as the second operand, the queries pass by as the first, 32
-// rows at a time through LDS (three tiles ahead, shared by the four wavefronts of a workgroup).  A lane then has one token
+// rows at a time through LDS (three tiles ahead, shared by the eight wavefronts of a workgroup).  A lane then has one token
 // (column l % 32) and half of the tile's queries in its registers, so the weights are summed in the lane: no exchange, no
 // atomics, one order of additions.  Rows as in chunk attention: token t of the chunk and head r of the group are row t R + r.
 //
-// Bounds: one query per sequence, the keys (8 x 16384 tokens of 8 KV heads over pages, 276 MB: 53 us, 5.2 TB/s); many, products
-// and exponentials (256 queries of 32 heads on 32768 tokens: 95 us, 720 TFLOP/s, matrix units busy 33 %, vector units 58 %).
+// Bounds: one query per sequence, the keys (8 x 16384 tokens of 8 KV heads, 276 MB: 46 us, 5.9 TB/s); many, products and
+// exponentials (256 queries of 32 heads on 32768 tokens: 88 us, 775 TFLOP/s; matrix units busy a third of the time, vector
+// units more than half).  Eight wavefronts to a workgroup, not four: a tile's load is one instruction to each of them (these two
+// 50 and 91 us with four, 4 x 8 heads with 5:1, 100 queries on 8000 tokens 51 against 57).
 #include "sik_mma.h"
 
 namespace sik {
 
 constexpr int kMassFull = 160;   // workgroups of 128 tokens below which four wavefronts share 32
+constexpr int kMassBlock = 512, kMassKeys = kMassBlock / kWave * 32;  // threads and tokens of a workgroup
 constexpr int kMassRows = 32;    // query rows of a tile
 constexpr int kMassBuffers = 4;  // tiles in LDS
 constexpr int kMassStage = 512;  // rows whose sums are in LDS at a time
@@ -28,7 +31,7 @@ struct MassArgs {
 };
 
 template <int DT>
-__global__ __launch_bounds__(kBlock, 4) void mass_kernel(const MassArgs a) {
+__global__ __launch_bounds__(kMassBlock, 4) void mass_kernel(const MassArgs a) {
     __shared__ struct {
         __align__(16) char q[kMassBuffers][kMassRows * 256];
         __align__(16) float lse[kMassStage];  // in powers of two; +infinity: the row contributes nothing
@@ -36,7 +39,7 @@ __global__ __launch_bounds__(kBlock, 4) void mass_kernel(const MassArgs a) {
     } lds;
     const int lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
     const int u = blockIdx.x / a.blocks, b = u / a.cv.Hkv, h = u % a.cv.Hkv;
-    const int key0 = (blockIdx.x % a.blocks) * (4 * 32);
+    const int key0 = (blockIdx.x % a.blocks) * kMassKeys;
     const int past = chunk_past(a.ch, b, a.cv.Lmax), nn = chunk_new(a.ch, b, past, a.cv.Lmax);
     const int end = past + nn;
     if (key0 >= end) return;
@@ -54,16 +57,11 @@ __global__ __launch_bounds__(kBlock, 4) void mass_kernel(const MassArgs a) {
     const int m0 = t_begin * a.R, rows = nn * a.R;
     const int tiles = t_begin < nn ? (rows - m0 + kMassRows - 1) / kMassRows : 0;
     const int64_t chunk_row = static_cast<int64_t>(b) * a.ch.n;
-    // (token, head) of the next tile's first row and of this lane's two rows of its loads (8 wv + 4 i + lane / 16); 32 rows on
-    // is a fixed step with at most one carry, no division
-    const int step_t = kMassRows / a.R, step_r = kMassRows % a.R;
-    int ft = t_begin, fr = 0, lt[2], lr[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int r = 8 * wv + 4 * i + (lane >> 4);
-        lt[i] = t_begin + r / a.R;
-        lr[i] = r % a.R;
-    }
+    // (token, head) of the next tile's first row and of this lane's row of its load; 32 rows on is a fixed step with at most one
+    // carry, no division
+    const int step_t = kMassRows / a.R, step_r = kMassRows % a.R, row = 4 * wv + (lane >> 4);
+    const uint32_t piece = ((lane & 15) ^ key_swizzle(row)) << 4;
+    int ft = t_begin, fr = 0, lt = t_begin + row / a.R, lr = row % a.R;
     auto advance = [&](int& t, int& r) {
         t += step_t;
         r += step_r;
@@ -72,22 +70,23 @@ __global__ __launch_bounds__(kBlock, 4) void mass_kernel(const MassArgs a) {
             ++t;
         }
     };
+    // where R divides 32, the rows of every full tile lie alike behind its first one
+    const int behind = lt - t_begin;
+    const uint32_t alike = (static_cast<uint32_t>(behind) * a.Hq + lr) * 256u + piece;
     auto load = [&](int tile) {
-        char* to = lds.q[tile % kMassBuffers];
         const uint16_t* base = dma_base(uniform(a.q + ((chunk_row + ft) * a.Hq + h * a.R) * kD));
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int row = 8 * wv + 4 * i + (lane >> 4);
-            const bool in = lt[i] < nn;  // rows beyond the end repeat the last one
-            const uint32_t off = (static_cast<uint32_t>((in ? lt[i] : nn - 1) - ft) * a.Hq + (in ? lr[i] : a.R - 1)) * 256u;
-            dma_16(base, off + (((lane & 15) ^ key_swizzle(row)) << 4),
-                   uniform(static_cast<int>(lds_offset(to) + (8 * wv + 4 * i) * 256)));
-            advance(lt[i], lr[i]);
+        uint32_t off = alike;
+        if (step_r != 0 || (tile + 1) * kMassRows > rows - m0) {
+            if (step_r == 0) lt = ft + behind;
+            const bool in = lt < nn;  // rows beyond the end repeat the last one
+            off = (static_cast<uint32_t>((in ? lt : nn - 1) - ft) * a.Hq + (in ? lr : a.R - 1)) * 256u + piece;
+            advance(lt, lr);
         }
+        dma_16(base, off, uniform(static_cast<int>(lds_offset(lds.q[tile % kMassBuffers]) + 4 * wv * 256)));
         advance(ft, fr);
     };
     auto stage = [&](int tile) {  // sums and last tokens of the next kMassStage rows
-        for (int i = threadIdx.x; i < kMassStage; i += kBlock) {
+        for (int i = threadIdx.x; i < kMassStage; i += kMassBlock) {
             const int m = m0 + tile * kMassRows + i, t = m / a.R;
             float l = __builtin_inff();
             if (m < rows) {
@@ -110,8 +109,8 @@ __global__ __launch_bounds__(kBlock, 4) void mass_kernel(const MassArgs a) {
             if (tile) __syncthreads();  // the sums staged before have been read
             stage(tile);
         }
-        if (tile + kMassBuffers - 1 <= tiles)  // two newer tiles of two loads each are on their way
-            dma_wait<2 * (kMassBuffers - 2)>();
+        if (tile + kMassBuffers - 1 <= tiles)  // two newer tiles are on their way, a load each
+            dma_wait<kMassBuffers - 2>();
         else
             dma_wait<0>();
         lds_reads_done();
@@ -245,19 +244,19 @@ hipError_t launch_mass(const Dims& d, const CacheView& c, const ChunkView& ch, c
                        const float* lse, int n_obs, const float* before, float* mass, hipStream_t s) {
     // shared tokens where the workgroups of 128 would leave compute units idle and there are queries for all four wavefronts:
     // 8 KV heads with 4:1 heads, 256 queries on 1000 tokens (64 workgroups) 15.4 us against 24.9, 2048 on the same 2048 (136)
-    // 133 against 167; but 64 on 4000 (256) 14.5 against 10.2
+    // 133 against 193; but 256 on 3500 (224) 34 against 30
     const int64_t wide = (d.Lmax + 127) / 128 * static_cast<int64_t>(d.units());
     const bool split = wide < kMassFull && static_cast<int64_t>(n_obs) * d.R > 2 * kMassRows;
-    const int blocks = split ? (d.Lmax + 31) / 32 : (d.Lmax + 127) / 128;
+    const int blocks = split ? (d.Lmax + 31) / 32 : (d.Lmax + kMassKeys - 1) / kMassKeys;
     const int64_t grid = static_cast<int64_t>(blocks) * d.units();
-    if (grid > 0x7fffffff / kBlock || static_cast<int64_t>(ch.n) * d.R > 0x7fffffff - kMassStage)
+    if (grid > 0x7fffffff / kMassBlock || static_cast<int64_t>(ch.n) * d.R > 0x7fffffff - kMassStage)
         return hipErrorInvalidConfiguration;
     const float sl2 = (scale > 0.0f ? scale : 1.0f / sqrtf(static_cast<float>(kD))) * 1.4426950408889634f;
     const MassArgs a{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(K), lse, c, ch, d.Hq, d.R, blocks, n_obs,
                      sl2, before, mass};
 #define SIK_MASS(DTV)                                                                                  \
     split ? launch_kernel(mass_split_kernel<DTV>, static_cast<int>(grid), kBlock, s, a)                 \
-          : launch_kernel(mass_kernel<DTV>, static_cast<int>(grid), kBlock, s, a)
+          : launch_kernel(mass_kernel<DTV>, static_cast<int>(grid), kMassBlock, s, a)
     return d.kv_dtype == kBF16 ? (SIK_MASS(kBF16)) : (SIK_MASS(kF16));
 #undef SIK_MASS
 }
