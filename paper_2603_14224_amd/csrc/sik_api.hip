@@ -129,7 +129,7 @@ const char* sik_strerror(int status) {
     }
 }
 
-int sik_version(void) { return 100; }
+int sik_version(void) { return 101; }
 
 int sik_plan_info(const sik_layout* layout, int32_t* info) {
     Dims d;

@@ -52,8 +52,7 @@ __device__ __forceinline__ void init_rows(RowState& st) {
     for (int c = 0; c < 4; ++c) st.o[c] = f32x16{};
 }
 
-// One tile of 32 NK tokens: `keys` and `values` are its LDS rows, s its logits.  PREC (binary32 outputs): what a weight loses
-// in 16 bits is kept as a second weight and a second product.
+// One tile of 32 NK tokens: `keys` are its LDS rows, s its logits.
 template <int DT, int NK>
 __device__ __forceinline__ void tile_logits(const char* keys, int lane, const u32x4 (&qf)[8], f32x16 (&s)[NK]) {
 #pragma unroll
@@ -100,7 +99,10 @@ __device__ __forceinline__ void rescale(RowState& st, float top) {
         for (int i = 0; i < 16; ++i) st.o[b][i] *= f;
 }
 
-// A tile's weights as operands, a group of 16 tokens in each; PREC: and what their rounding dropped.
+// A tile's weights as operands, a group of 16 tokens in each.  The matrix units take both operands in the values' type, so a
+// weight is rounded to 16 bits, by at most 2^-8 (bf16) or 2^-11 (fp16; below 2^-14 by 2^-25) of itself, half of its step, up or
+// down, so that a row's result is off by about as much as by its own rounding to that type.  The sum that divides it is taken
+// before the rounding.  PREC (binary32 results): what the rounding dropped is a second operand.
 template <int NK, bool PREC>
 struct Weights {
     u32x4 w[2 * NK], rest[PREC ? 2 * NK : 1];

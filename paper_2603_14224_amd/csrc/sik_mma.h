@@ -60,7 +60,8 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p) {
 // 64 x 16 B from base + off (bytes, per lane) to LDS [to, to + 1 KB).  Written in assembly because the compiler would wait
 // for it before every LDS read that follows; dma_wait is the wait.  A base may come from a vector instruction
 // (readfirstlane), and a memory instruction may read such a scalar register only five states later: dma_base sees to that,
-// which the compiler does not do for assembly.
+// which the compiler does not do for assembly.  (m0 holds nothing across instructions here: the compiler sets it right before
+// a use of its own, and these kernels have none.)
 template <class T>
 __device__ __forceinline__ T* dma_base(T* base) {
     asm volatile("s_nop 4" : "+s"(base));

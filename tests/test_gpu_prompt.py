@@ -396,6 +396,23 @@ def test_evict(B, Hkv, lengths, n_keep, n_sink, n_recent, page, dtype, kind):
     assert torch.equal(only, keep) and torch.equal(alone, mo)
 
 
+def test_tensors_on_another_device_are_refused():
+    lay = sik.make_layout(1, 1, 2, D, 64, BF)
+    K = torch.zeros(1, 1, 64, D, dtype=BF, device="cuda")
+    q, out = torch.zeros(1, 4, 2, D, dtype=BF, device="cuda"), torch.zeros(1, 4, 2, D, dtype=BF, device="cuda")
+    ws = sik.alloc_chunk_workspace(lay, 4)
+    with pytest.raises(ValueError, match="seq_len"):
+        sik.make_chunk(4, torch.zeros(1, dtype=torch.int32))
+    chunk = sik.make_chunk(4, ints([3]))
+    for bad in (dict(q=q.cpu()), dict(K=K.cpu()), dict(out=out.cpu()), dict(ws=ws.cpu()), dict(lse=torch.zeros(1, 4, 2))):
+        a = {**dict(q=q, K=K, out=out, ws=ws, lse=None), **bad}
+        with pytest.raises(ValueError, match="is on"):
+            sik.sik_chunk_attn(lay, chunk, a["q"], a["K"], K, 0.0, a["out"], a["lse"], a["ws"])
+    with pytest.raises(ValueError, match="positions is on"):
+        sik.sik_rope_append(lay, chunk, q, q[:, :, :1].contiguous(), out, k_out=torch.zeros_like(q[:, :, :1].contiguous()),
+                            positions=torch.zeros(1, 4, dtype=torch.int32))
+
+
 # --------------------------------------------------------------------------------------------- together
 
 def serve(stream=None, page=0, dtype=BF):
