@@ -538,3 +538,96 @@ def test_streams_and_graphs():
             torch.cuda.synchronize()
             for x, w in zip(("out", "lse", "mass", "keep"), st["want"]):
                 assert torch.equal(st[x], w)
+
+
+# --------------------------------------------------------------------------------------------- calls at the edges
+
+def test_rope_batch_of_single_tokens_in_a_graph():
+    # the rows of a decode step, out of a fused projection, captured and replayed with other inputs and lengths in between
+    gen = gen_of(31)
+    B, Hkv, Hq = 3, 2, 8
+    lay = sik.make_layout(B, Hkv, Hq, D, 4096, BF)
+    qkv, lens = randn((B, 1, (Hq + 2 * Hkv) * D), gen, BF), ints([5, 0, 4095])
+    q, k, _ = (x.unflatten(2, (-1, D)) for x in qkv.split([Hq * D, Hkv * D, Hkv * D], 2))
+    freq = (10000.0 ** (-torch.arange(0, D, 2, device="cuda").double() / D)).float()
+    q_out, k_out = torch.zeros(B, 1, Hq, D, dtype=BF, device="cuda"), torch.zeros(B, 1, Hkv, D, dtype=BF, device="cuda")
+    chunk = sik.make_chunk(1, lens)
+    call = lambda: sik.sik_rope_append(lay, chunk, q, k, q_out, k_out=k_out, inv_freq=freq)
+    call()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for i in range(4):
+        qkv.copy_(randn(qkv.shape, gen, BF))
+        lens.copy_(ints([5 + i, 4095 - i, 100 * i]))
+        q_out.zero_(), k_out.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for b, at in enumerate([5 + i, 4095 - i, 100 * i]):
+            for got, x in ((q_out[b], q[b]), (k_out[b], k[b])):
+                ref, size = rope64(x, None, 0, torch.tensor([at], device="cuda"), freq, False)
+                assert ((got.double() - ref).abs() <= rope_tolerance(ref, size, BF)).all()
+
+
+def test_two_streams_at_once_and_a_shared_prefix():
+    # two sequences that share their first two pages; two calls at once with a workspace each; a scale of their own
+    gen = gen_of(41)
+    B, Hkv, Hq, n, past, page = 2, 2, 10, 30, 400, 32
+    c = Cache(B, Hkv, past + n, FP, page, [past + n, past + 7], gen)
+    c.table[1, :2] = c.table[0, :2]
+    lay = sik.make_layout(B, Hkv, Hq, D, past + n, FP, torch.float32)
+    torch.cuda.synchronize()
+    streams, res = [torch.cuda.Stream() for _ in range(2)], []
+    for s, scale in zip(streams, (0.3, 0.05)):
+        with torch.cuda.stream(s):
+            q = randn((B, n, Hq, D), torch.Generator(device="cuda").manual_seed(3), FP)
+            out, lse = run_chunk(lay, c, q, [past, past], [n, 7], n, scale=scale)
+            mass = torch.zeros(B, Hkv, past + n, device="cuda")
+            chunk = sik.make_chunk(n, ints([past, past]), n_new=ints([n, 7]), pages=c.pages)
+            sik.sik_attn_mass(lay, chunk, q, c.K, scale, lse, n, None, mass)
+            res.append((q, out, lse, mass, scale, chunk))
+    torch.cuda.synchronize()
+    for q, out, lse, mass, scale, _ in res:
+        check_chunk(c, q, [past, past], [n, 7], out, lse, scale=scale)
+        for b, m in enumerate((n, 7)):
+            k, there = c.rows(c.K, b, past + m)
+            r = attn64(q[b, :m], k, None, there, past, scale)
+            want, tol = mass64(r, lse[b, :m], n)
+            assert ((mass[b, :, :past + m].double() - want).abs() <= tol + want * 2 ** -23).all()
+
+
+def test_longest_cache():
+    # max_len at its limit: one query over 4 128 768 tokens, most of them zeros; the weights; the eviction by other weights
+    L = 4128768
+    gen = gen_of(51)
+    lay = sik.make_layout(1, 1, 2, D, L, BF, torch.float32)
+    K, V = (torch.zeros(1, 1, L, D, dtype=BF, device="cuda") for _ in range(2))
+    rows = torch.cat([torch.arange(100), torch.arange(L - 50, L)]).cuda()
+    for x in (K, V):
+        x[0, 0, rows] = randn((150, D), gen, BF)
+    q = randn((1, 1, 2, D), gen, BF) * 4
+    chunk = sik.make_chunk(1, ints([L - 1]))
+    out, lse = torch.zeros(1, 1, 2, D, device="cuda"), torch.zeros(1, 1, 2, device="cuda")
+    ws = sik.alloc_chunk_workspace(lay, 1)
+    sik.sik_chunk_attn(lay, chunk, q, K, V, 0.0, out, lse, ws)
+    mass = torch.zeros(1, 1, L, device="cuda")
+    sik.sik_attn_mass(lay, chunk, q, K, 0.0, lse, 1, None, mass)
+    z = q[0, 0].double() @ K[0, 0, rows].double().T * SCALE
+    m = z.amax(-1, keepdim=True).clamp(min=0)
+    p = torch.exp(z - m)
+    l = p.sum(-1, keepdim=True) + (L - 150) * torch.exp(-m)
+    ref, spread = (p @ V[0, 0, rows].double()) / l, (p @ V[0, 0, rows].double().abs()) / l
+    # logits as in the tests above, |q| |k| up to 4 * 128 * 4; sums of at most 2^14 terms of like size in each of the parts
+    rel = 2 * 132 * 2 ** -23 * 2048 * SCALE + 2 ** 14 * 2 ** -23
+    assert ((out[0, 0].double() - ref).abs() <= spread * rel + 1e-12).all()
+    assert ((lse[0, 0].double() - (m + l.log())[:, 0]).abs() <= rel).all()
+    assert (mass[0, 0, 200].double() - torch.exp(-lse[0, 0].double()).sum()).abs() <= mass[0, 0, 200].double() * 2 ** -19
+    assert torch.equal(mass[0, 0, 200:300], mass[0, 0, 200].expand(100))
+
+    w = torch.exp(torch.randn(1, 1, L, generator=gen, device="cuda")).round(decimals=3)
+    keep = torch.zeros(1, 1, 100000, dtype=torch.int32, device="cuda")
+    sik.sik_evict(lay, w, ints([L]), 100000, keep, ws, n_sink=3, n_recent=1000)
+    best = torch.sort(w[0, 0, 3:L - 1000], descending=True, stable=True)[1][:100000 - 1003] + 3
+    want = torch.cat([torch.arange(3).cuda(), best.sort()[0], torch.arange(L - 1000, L).cuda()])
+    assert torch.equal(keep[0, 0].long(), want)
