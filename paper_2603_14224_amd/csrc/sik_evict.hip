@@ -7,16 +7,19 @@
 // up, finds the cut's bin and writes its tokens of that bin, a few per cent, behind those of the chunks before), `place` (the
 // other two digits from those tokens alone, then the chunk's part of the list).
 //
-// Bounds: the list, chains of memory, counting and barriers (32 rows of 65536 weights in 34 us, of which 5, 6 and 8 inside the
-// launches; 256 rows of 16370 in 23); the rows, memory (2048 rows of K and V for each of 256, 537 MB: 92 us, 5.9 TB/s).
+// Bounds: the list, chains of memory, counting and barriers (one row of 65536 weights in 19.5 us, 32 of them in 31; 256 rows of
+// 16370 in 23); the rows, memory (2048 rows of K and V for each of 256, 537 MB: 87 us, 6.2 TB/s).
 #include "sik_chunk.h"
 
 namespace sik {
 
 constexpr int kEvictBlock = 1024;
 constexpr int kDigitBins = 2048;   // of the first two digits; the last one has 1024
-constexpr int kChunkTokens = 8192; // tokens of a chunk, more where there would be more than kEvictChunks of them
-constexpr int kEvictChunks = 64;
+constexpr int kChunkTokens = 4096; // the fewest tokens of a chunk
+constexpr int kEvictChunks = 64;   // the most chunks of a row, whose counts every workgroup adds up
+// Compute units.  A second round of workgroups costs more than longer chunks: 32 rows of 65544 weights in nine chunks of 8192
+// took 39 us, in eight of 8256 31.
+constexpr int kEvictUnits = 256;
 constexpr int kEvictStep = 4096;   // tokens of a workgroup at four weights per thread
 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));  // rows start at any multiple of 4 bytes
@@ -203,11 +206,11 @@ struct EvictScratch {
     int64_t list_len;
 };
 
-// A wavefront's consecutive part of a chunk, [first, last) in steps of 256 tokens, four per lane.  The first steps (all of them
-// where a chunk has kChunkTokens) are requested before anything else is known, lengths included, so that a launch waits for
-// memory once: a step's weights then come from registers however often they are looked at.
+// A wavefront's consecutive part of a chunk, [first, last) in steps of 256 tokens, four per lane.  The first two steps are
+// requested before anything else is known, lengths included, so that a launch waits for memory once where these are all: a
+// step's weights then come from registers however often they are looked at.
 struct PartWeights {
-    static constexpr int kHeld = kChunkTokens / (kEvictBlock / kWave) / 256;
+    static constexpr int kHeld = 2;
     const float* m;
     int Lmax, lane, start, len, first, last;
     f32x4_any held[kHeld];
@@ -216,7 +219,7 @@ struct PartWeights {
         lane = threadIdx.x & 63;
         start = c * w.per + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * len;
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k) held[k] = load4(m, start + 256 * k + 4 * lane, Lmax);
+        for (int k = 0; k < kHeld; ++k) held[k] = load4(m, start + 256 * k + 4 * lane, 256 * k < len ? Lmax : 0);
     }
     __device__ __forceinline__ void end_at(int L) {
         first = min(start, L);
@@ -452,19 +455,24 @@ __global__ __launch_bounds__(kBlock) void evict_rows_kernel(EvictArgs a, CacheVi
     }
 }
 
-// One workgroup per row (us for 1 / 128 / 256 rows against the three launches): 16370 tokens 20.7 / 21.9 / 22.9 against 21.1 /
-// 24.0 / 39.6; beyond 16384 only where the rows fill half of the chip: 20000 tokens 25 / 26.0 / 27.1 against 21.4 / 38.5 /
-// 54.6, 32000 38.5 / 40.2 / 42.2 against 21.5 / 41.4 / 73.7.
+// One workgroup per row up to 12288 tokens, up to 32768 from as many rows on as the chip has no room to split (us against the
+// three launches): 12000 tokens, 1 row 17.1 / 17.5, 256 rows 18.5 / 28.6; 16370, 1 row 21.0 / 17.6, 64 rows 21.4 / 21.2, 256
+// rows 22.9 / 35.2; 20000, 128 rows 25.5 / 28.9; 24000, 128 rows 30 / 29.9, 256 rows 31 / 45; 32000, 128 rows 40 / 35, 256
+// rows 42 / 58.
 static bool evict_direct(const Dims& d) {
-    return d.Lmax <= 4 * kEvictStep || (d.Lmax <= 8 * kEvictStep && d.units() >= 128);
+    const int steps = (d.Lmax + kEvictStep - 1) / kEvictStep;
+    return steps <= 3 || (steps <= 8 && d.units() >= (steps <= 5 ? 64 : steps <= 6 ? 128 : 192));
 }
 
 static EvictScratch evict_plan(const Dims& d, void* ws, size_t* bytes) {
     EvictScratch w{};
-    w.per = kChunkTokens;
-    const int least = (d.Lmax + kEvictChunks - 1) / kEvictChunks;
-    if (least > w.per) w.per = (least + 4095) / 4096 * 4096;
-    w.chunks = evict_direct(d) ? 0 : (d.Lmax + w.per - 1) / w.per;
+    if (!evict_direct(d)) {
+        const int by_units = kEvictUnits / d.units(), by_len = (d.Lmax + kChunkTokens - 1) / kChunkTokens;
+        w.chunks = by_units < 1 ? 1 : by_units < kEvictChunks ? by_units : kEvictChunks;
+        if (w.chunks > by_len) w.chunks = by_len;
+        w.per = ((d.Lmax + w.chunks - 1) / w.chunks + 63) / 64 * 64;  // four tokens to a lane of each of 16 wavefronts
+        w.chunks = (d.Lmax + w.per - 1) / w.per;
+    }
     w.list_len = d.Lmax;
     const int64_t units = d.units(), rows = units * w.chunks;
     uint32_t* p = static_cast<uint32_t*>(ws);
