@@ -416,6 +416,8 @@ def _head_rows(name, t, dtype, dev, shape):
     stride = s1 if n > 1 else s0 if B > 1 else heads * D
     if s3 != 1 or (heads > 1 and s2 != D) or (B > 1 and s0 != n * stride):
         raise ValueError(f"{name}: head rows of a token must be contiguous and tokens evenly spaced")
+    if stride < heads * D:  # a broadcast row has the stride 0, which to the C side means packed rows
+        raise ValueError(f"{name}: tokens overlap (one every {stride} elements, {heads * D} needed)")
     if t.get_device() != dev:
         raise ValueError(f"{name} is on {t.device}, the call runs on device {dev}")
     return t.data_ptr(), stride

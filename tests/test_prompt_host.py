@@ -151,3 +151,28 @@ def test_binding_checks_types_and_shapes():
                       pages=sik.make_pages(table, 16, 4))
     with pytest.raises(ValueError):
         sik.sik_evict(lay, torch.zeros(2, 2, 64), lens, 8, torch.zeros(2, 2, 9, dtype=torch.int32), None)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the tensors below are the CPU's")
+@pytest.mark.parametrize("name", ["q", "k", "v"])
+@pytest.mark.parametrize("B,n,own", [(1, 4, (1, 1)), (3, 1, (1, 1)), (3, 4, (1, 1)), (3, 4, (3, 1)), (3, 4, (1, 4))])
+def test_broadcast_rows_are_refused(name, B, n, own):
+    # one row for several tokens or sequences: a stride of 0, which to the C side means packed rows, of which there are more
+    lay, heads = L(batch=B, max_len=64), dict(q=8, k=2, v=2)
+    a = {x: torch.zeros(B, n, h, 128, dtype=torch.bfloat16) for x, h in heads.items()}
+    a[name] = torch.zeros(*own, heads[name], 128, dtype=torch.bfloat16).expand(B, n, -1, -1)
+    K, V = (torch.zeros(B, 2, 64, 128, dtype=torch.bfloat16) for _ in range(2))
+    chunk = sik.make_chunk(n, torch.zeros(B, dtype=torch.int32))
+    with pytest.raises(ValueError, match=f"^{name}: "):
+        sik.sik_rope_append(lay, chunk, a["q"], a["k"], torch.zeros_like(a["q"], memory_format=torch.contiguous_format),
+                            v=a["v"], K=K, V=V)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the tensors below are the CPU's")
+def test_overlapping_tokens_are_refused():
+    lay = L(batch=1, max_len=64)
+    k = torch.zeros(1, 4, 2, 128, dtype=torch.bfloat16)
+    q = torch.zeros(4096, dtype=torch.bfloat16).as_strided((1, 4, 8, 128), (4096, 512, 128, 1))
+    with pytest.raises(ValueError, match="^q: "):
+        sik.sik_rope_append(lay, sik.make_chunk(4, torch.zeros(1, dtype=torch.int32)), q, k, torch.zeros(1, 4, 8, 128, dtype=torch.bfloat16),
+                            k_out=torch.zeros_like(k))
