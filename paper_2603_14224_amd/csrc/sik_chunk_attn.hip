@@ -23,9 +23,19 @@ namespace sik {
 constexpr int kRowsTile = 128;   // rows of a workgroup of the `rows` form
 constexpr int kTokensTile = 32;  // of the `tokens` form
 constexpr int kMaxParts = 128;   // workgroups that share one row tile's cache
-// A row's reference maximum moves only when a logit exceeds it by more than this (in powers of two): weights stay below 256
-// and the 64 registers of the output are rescaled a few times per pass instead of once per tile.
-constexpr float kSlack = 8.0f;
+// A row's weights are exp2(logit - m).  The reference m moves only when a tile's largest logit leaves a band around it, so that
+// the 64 registers of the output are rescaled a few times per pass instead of once per tile.
+//   bf16: m is a maximum that was, and moves up when a logit exceeds it by more than kSlack: weights stay below 2^8, and what is
+//   far below keeps its 8 bits, as the type has the exponents of binary32.
+//   fp16 has few exponents: below 2^-14 a weight is held to 2^-25 only, and where one token outweighs thousands of others by
+//   that much (a sink), all of them would vanish from the sum of the values but not from the sum of the weights.  So m lies
+//   2^kUnder below the largest logit, and moves down as well, to the largest logit of a tile that is more than 2^kDrop (binary32
+//   results: kDropPrec) below: a tile's largest weight is then at least 2^(kUnder - kDrop), and what the tile's 64 tokens lose
+//   at the lower end is at most 2^-14 (2^-18) of that one.  At most 2^kDepth down from the highest reference: a row of 2^22 tokens
+//   of weights below 2^(15 + kDepth) and values below 2^16 stays within binary32.  These references are whole numbers, so that
+//   moving one, any number of times, rounds nothing.  The downward moves cost 1 % of a prompt's time (2048 tokens behind 6144,
+//   8/32 heads: 258 us against 255) and 4 % with binary32 results (353 against 340; 366 with kDropPrec 4, 356 with 6).
+constexpr float kSlack = 8.0f, kUnder = 7.0f, kDrop = 12.0f, kDropPrec = 8.0f, kDepth = 60.0f;
 
 struct ChunkAttn {
     const uint16_t *q, *K, *V;
@@ -42,11 +52,12 @@ struct ChunkAttn {
 // A wavefront's 32 rows: one query per lane (both halves hold the same), output registers [channel block][16].
 struct RowState {
     float m, l;
+    float hi;  // fp16: the highest m so far
     f32x16 o[4];
 };
 
 __device__ __forceinline__ void init_rows(RowState& st) {
-    st.m = kNegBig;
+    st.m = st.hi = kNegBig;
     st.l = 0.0f;
 #pragma unroll
     for (int c = 0; c < 4; ++c) st.o[c] = f32x16{};
@@ -89,8 +100,26 @@ __device__ __forceinline__ float tile_top(const f32x16 (&s)[NK], float c) {
     return fmaxf(lo, hi) * c;
 }
 
+// Does the row's reference have to move before a tile whose largest logit is top (-infinity: none counts)?
+template <int DT, bool PREC>
+__device__ __forceinline__ bool has_to_move(const RowState& st, float top) {
+    if constexpr (DT != kF16) return top > st.m + kSlack;
+    constexpr float low = kUnder - (PREC ? kDropPrec : kDrop);
+    return top > st.m + kUnder + kSlack || (top > kNegBig && fmaxf(top, st.hi - kDepth + kUnder) < st.m + low);
+}
+
+template <int DT, bool PREC>
 __device__ __forceinline__ void rescale(RowState& st, float top) {
-    const float m = fmaxf(st.m, top), f = fast_exp2(st.m - m);
+    float m, f;
+    if constexpr (DT != kF16) {
+        m = fmaxf(st.m, top);
+        f = fast_exp2(st.m - m);
+    } else {
+        m = ceilf(top) - kUnder;
+        m = m > st.m ? m : has_to_move<DT, PREC>(st, top) ? fmaxf(m, st.hi - kDepth) : st.m;
+        f = __builtin_amdgcn_ldexpf(1.0f, static_cast<int>(fmaxf(st.m - m, -200.0f)));
+        st.hi = fmaxf(st.hi, m);
+    }
     st.m = m;
     st.l *= f;
 #pragma unroll
@@ -100,9 +129,11 @@ __device__ __forceinline__ void rescale(RowState& st, float top) {
 }
 
 // A tile's weights as operands, a group of 16 tokens in each.  The matrix units take both operands in the values' type, so a
-// weight is rounded to 16 bits, by at most 2^-8 (bf16) or 2^-11 (fp16; below 2^-14 by 2^-25) of itself, half of its step, up or
-// down, so that a row's result is off by about as much as by its own rounding to that type.  The sum that divides it is taken
-// before the rounding.  PREC (binary32 results): what the rounding dropped is a second operand.
+// weight is rounded to 16 bits, by at most 2^-8 (bf16) or 2^-11 (fp16; below 2^-14 by 2^-25, see the references above) of itself,
+// half of its step, up or down, so that a row's result is off by about as much as by its own rounding to that type (both together,
+// root mean square over prompts of random rows: bf16 2.1e-3 of the result, 1.6e-3 of it the result's own; fp16 2.9e-4 and 2.1e-4;
+// a second operand for the rest takes 1.35 times as long).  The sum that divides it is taken before the rounding.  PREC (binary32
+// results): what the rounding dropped is a second operand.
 template <int NK, bool PREC>
 struct Weights {
     u32x4 w[2 * NK], rest[PREC ? 2 * NK : 1];
@@ -248,7 +279,7 @@ __global__ __launch_bounds__(kBlock, 2) void chunk_rows_kernel(const ChunkAttn a
         if (tile * kTile + kTile - 1 > past + first_t || mapped != 15u)
             mask_logits<2>(s, lane, past + t - tile * kTile, mapped);
         top = tile_top<2>(s, a.scale_log2e);
-        return __any(top > st.m + kSlack) != 0;
+        return __any(has_to_move<DT, ODT == kF32>(st, top)) != 0;
     };
     // one tile, whose logits are s; the next one's to n; true: the maximum has to move before they can be used
     auto step = [&](const f32x16(&s)[2], f32x16(&n)[2], int tile) {
@@ -276,7 +307,7 @@ __global__ __launch_bounds__(kBlock, 2) void chunk_rows_kernel(const ChunkAttn a
         moved = masked_top(s, tile);
     }
     while (tile < tw) {
-        if (moved) rescale(st, top);
+        if (moved) rescale<DT, ODT == kF32>(st, top);
         // (left only where the maximum moves: the output registers stay where they are while it does not)
         for (moved = false; tile < tw && !moved;) {
             moved = step(s, n, tile++);
@@ -389,7 +420,7 @@ __global__ __launch_bounds__(kBlock, 2) void chunk_tokens_kernel(const ChunkAttn
         else
             dma_wait<0>();
         const float top = tile_top<1>(s, a.scale_log2e);
-        if (__any(top > st.m + kSlack)) rescale(st, top);
+        if (__any(has_to_move<DT, ODT == kF32>(st, top))) rescale<DT, ODT == kF32>(st, top);
         Weights<1, ODT == kF32> w;
         tile_weights<DT, 1>(st, s, a.scale_log2e, w);
         tile_values<DT, 1>(st, w, values, lane);

@@ -118,3 +118,24 @@ def keep64(mass, length, n_keep, n_sink, n_recent):
 
 
 SCALE = 1.0 / math.sqrt(D)
+
+
+def out_tolerance_by_tile(r, v, dtype, out_dtype):
+    """As out_tolerance, but for what fp16 weights lose: not 2^-25 of the row's largest for each token, but of the largest of
+    the token's own 64, which is held at 2^-5 or more (binary32 results: 2^-1), and 2^-90 of the row's where a tile lies too deep
+    for that.  v [Hkv, L, D]."""
+    Hkv, R, n, L = r["z"].shape
+    w = torch.exp(r["z"] - torch.logsumexp(r["z"], -1, keepdim=True)).nan_to_num(0.0)
+    lost = torch.zeros_like(w)
+    if dtype == torch.float16:
+        top = torch.nn.functional.pad(w, (0, -L % 64)).unflatten(-1, (-1, 64)).amax(-1, keepdim=True).expand(-1, -1, -1, -1, 64)
+        lost = top.flatten(-2)[..., :L] * (2 ** -24 if out_dtype == torch.float32 else 2 ** -20) + 2 ** -90
+        lost = torch.where(r["ok"], lost, 0.0)
+    eps = torch.finfo(dtype).eps
+    half = eps / 2 if out_dtype != torch.float32 else eps * eps / 4
+    rel = (half + 2 * r["dz"][..., None] + (r["L"] + 16) * 2 ** -23)
+    lost = torch.matmul(lost.view(Hkv, R * n, L), v.double().abs()).view(Hkv, R, n, D).permute(2, 0, 1, 3).reshape(n, Hkv * R, D)
+    tol = r["spread"] * rel + lost + r["out"].abs() * 2 ** -22
+    if out_dtype != torch.float32:
+        tol = tol + r["out"].abs() * eps / 2 * (1 + 2 ** -8) + tol * eps + (2 ** -25 if dtype == torch.float16 else 0.0)
+    return tol + 1e-37

@@ -7,7 +7,7 @@ import torch
 
 import paper_2603_14224_amd as sik
 from prompt_reference import (D, SCALE, attn64, gather_cache, keep64, lse_tolerance, mass64, out_tolerance, rope64,
-                              rope_tolerance)
+                              out_tolerance_by_tile, rope_tolerance)
 
 pytestmark = pytest.mark.gpu
 BF, FP = torch.bfloat16, torch.float16
@@ -631,3 +631,73 @@ def test_longest_cache():
     best = torch.sort(w[0, 0, 3:L - 1000], descending=True, stable=True)[1][:100000 - 1003] + 3
     want = torch.cat([torch.arange(3).cuda(), best.sort()[0], torch.arange(L - 1000, L).cuda()])
     assert torch.equal(keep[0, 0].long(), want)
+
+
+# --------------------------------------------------------------------------------------------- rows that few tokens dominate
+
+def check_by_tile(c, q, past, out, lse):
+    for b in range(q.shape[0]):
+        L = past + q.shape[1]
+        k, there = c.rows(c.K, b, L)
+        v, _ = c.rows(c.V, b, L)
+        r = attn64(q[b], k, v, there, past, SCALE)
+        off = (out[b].double() - r["out"]).abs() / out_tolerance_by_tile(r, v, q.dtype, out.dtype)
+        assert off.max() <= 1, (b, float(off.max()))
+        assert ((lse[b].double() - r["lse"]).abs() <= lse_tolerance(r)).all()
+
+
+def dominated(L, n, Hkv, R, dtype, page, sinks, gen, spread=0.5):
+    """A cache in which the tokens `sinks` {token: nats} outweigh all others, by so many nats, and have values of zero with the
+    64 around them, so that a row is what the others give; the query heads of a group see them in shares of 1, 1/2, 1/4 .. of
+    that."""
+    c = Cache(1, Hkv, L, dtype, page, [L], gen)
+    k, v = torch.randn(2, Hkv, L, D, generator=gen, device="cuda")
+    k[..., 0] = 0
+    for at, nats in sinks.items():
+        k[:, at] = 0
+        k[:, at, 0] = nats
+        v[:, at // 64 * 64:at // 64 * 64 + 64] = 0
+    c.write(c.K, 0, 0, k.to(dtype))
+    c.write(c.V, 0, 0, v.to(dtype))
+    q = torch.randn(1, n, Hkv * R, D, generator=gen, device="cuda") * spread
+    q[..., 0] = math.sqrt(D) * 0.5 ** torch.arange(R, device="cuda").repeat(Hkv)
+    return c, q.to(dtype)
+
+
+@pytest.mark.parametrize("nats", [12, 16, 18, 24, 38])
+@pytest.mark.parametrize("n,past,page", [(1, 32767, 0), (3, 4096, 64), (40, 20000, 0), (130, 900, 16)])
+@pytest.mark.parametrize("dtype,out_dtype", [(FP, FP), (FP, torch.float32), (BF, torch.float32)])
+def test_chunk_attn_one_token_far_above_the_others(nats, n, past, page, dtype, out_dtype):
+    # a sink at the front: each of the others has a weight of exp(-nats), all of them together are the row's values
+    c, q = dominated(past + n, n, 2, 2, dtype, page, {0: nats}, gen_of(nats, n))
+    lay = sik.make_layout(1, 2, 4, D, past + n, dtype, out_dtype)
+    out, lse = run_chunk(lay, c, q, [past], None, n)
+    check_by_tile(c, q, past, out, lse)
+
+
+@pytest.mark.parametrize("n,past,page", [(1, 6000, 16), (9, 2500, 0), (70, 3000, 32)])
+@pytest.mark.parametrize("dtype,out_dtype", [(FP, FP), (FP, torch.float32), (BF, torch.float32)])
+def test_chunk_attn_references_up_and_down(n, past, page, dtype, out_dtype):
+    # dominating tokens all along the cache, higher and lower in turn, the highest in the middle, beyond the depth of a reference
+    heights = [20, 3, 31, 9, 14, 70, 26, 5, 41, 11]
+    sinks = {at: heights[i % 10] if at != 1300 else 95 for i, at in enumerate(range(20, past, 160))}
+    c, q = dominated(past + n, n, 1, 4, dtype, page, sinks, gen_of(n, 3), spread=0.3)
+    lay = sik.make_layout(1, 1, 4, D, past + n, dtype, out_dtype)
+    out, lse = run_chunk(lay, c, q, [past], None, n)
+    check_by_tile(c, q, past, out, lse)
+
+
+@pytest.mark.parametrize("n,past", [(1, 4095), (3, 30000), (50, 2000)])
+@pytest.mark.parametrize("dtype,out_dtype", [(FP, FP), (FP, torch.float32), (BF, torch.float32)])
+def test_chunk_attn_far_tokens_of_an_unsplit_cache(n, past, dtype, out_dtype):
+    # as many sequences as fill the chip, on the same pages: one workgroup has the sink and all that is far below it
+    B, Hkv, R = 40, 8, 4
+    nats = 25 if out_dtype == torch.float32 else 17  # (fp16 results end at 2^-24)
+    c, q = dominated(past + n, n, Hkv, R, dtype, 64, {70: nats}, gen_of(n, 9))
+    c.table = c.table.expand(B, -1).contiguous()
+    c.pages = sik.make_pages(c.table, 64, c.K.shape[0])
+    lay = sik.make_layout(B, Hkv, Hkv * R, D, past + n, dtype, out_dtype)
+    out, lse = run_chunk(lay, c, q.expand(B, -1, -1, -1).contiguous(), [past] * B, None, n)
+    check_by_tile(c, q, past, out[7:8], lse[7:8])
+    for x in (out, lse):
+        assert torch.equal(x, x[7:8].expand_as(x))
