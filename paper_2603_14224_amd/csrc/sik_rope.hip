@@ -38,15 +38,12 @@ __global__ __launch_bounds__(kBlock) void rope_kernel(RopeArgs a, CacheView cv, 
     const bool rotated = 8 * p < a.rotary_dim;
     const bool upper = !PAIRS && 8 * p >= half;                          // second channels of their pairs
     const int po = !rotated ? p : PAIRS ? p : upper ? p - half / 8 : p + half / 8;  // lane with the partners
-    float sn[PAIRS ? 4 : 8], cs[PAIRS ? 4 : 8];
+    float sn[PAIRS ? 4 : 8], cs[PAIRS ? 4 : 8];  // (of rotated channels)
     if (rotated) {
         const int position = a.positions ? a.positions[src] : past + t;
         const float* f = a.inv_freq + (PAIRS ? 4 * p : 8 * (upper ? po : p));
 #pragma unroll
         for (int e = 0; e < (PAIRS ? 4 : 8); ++e) turn(position, f[e], sn[e], cs[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < (PAIRS ? 4 : 8); ++e) sn[e] = 0.0f, cs[e] = 1.0f;
     }
 
     for (int it = 0; it < steps; ++it) {
@@ -85,14 +82,19 @@ __global__ __launch_bounds__(kBlock) void rope_kernel(RopeArgs a, CacheView cv, 
                 }
             }
             float yo[8];
+            if (rotated) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if constexpr (PAIRS) {
-                    const float s = (e & 1) ? sn[e >> 1] : -sn[e >> 1];
-                    yo[e] = fmaf(xo[e], cs[e >> 1], xo[e ^ 1] * s);
-                } else {
-                    yo[e] = fmaf(xo[e], cs[e], xp[e] * (upper ? sn[e] : -sn[e]));
+                for (int e = 0; e < 8; ++e) {
+                    if constexpr (PAIRS) {
+                        const float s = (e & 1) ? sn[e >> 1] : -sn[e >> 1];
+                        yo[e] = fmaf(xo[e], cs[e >> 1], xo[e ^ 1] * s);
+                    } else {
+                        yo[e] = fmaf(xo[e], cs[e], xp[e] * (upper ? sn[e] : -sn[e]));
+                    }
                 }
+            } else {  // (not by a sine of zero: an infinity has to stay one, and beside its neighbour)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) yo[e] = xo[e];
             }
             uint32_t o[4];
 #pragma unroll

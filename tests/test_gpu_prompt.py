@@ -633,6 +633,34 @@ def test_longest_cache():
     assert torch.equal(keep[0, 0].long(), want)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("rotary", [0, 32, 96])
+def test_rope_channels_that_are_not_rotated_pass_through(interleaved, dtype, rotary):
+    # infinities and NaN among them too, each beside finite neighbours, into rows and into a cache
+    gen = gen_of(rotary, 61)
+    B, Hkv, Hq, n, past = 1, 2, 4, 9, 3
+    q, k, v = (randn((B, n, h, D), gen, dtype) for h in (Hq, Hkv, Hkv))
+    for x in (q, k, v):
+        for i, odd in enumerate((math.inf, -math.inf, math.nan)):
+            x[..., rotary + 5 * i::16] = odd
+    freq = (10000.0 ** (-torch.arange(0, rotary, 2, device="cuda").double() / max(rotary, 1))).float() if rotary else None
+    lay = sik.make_layout(B, Hkv, Hq, D, past + n, dtype)
+    chunk = sik.make_chunk(n, ints([past]))
+    q_out, k_out = torch.zeros_like(q), torch.zeros_like(k)
+    K, V = (torch.zeros(B, Hkv, past + n, D, dtype=dtype, device="cuda") for _ in range(2))
+    sik.sik_rope_append(lay, chunk, q, k, q_out, k_out=k_out, inv_freq=freq, interleaved=interleaved)
+    sik.sik_rope_append(lay, chunk, q, k, q_out, v=v, K=K, V=V, inv_freq=freq, interleaved=interleaved)
+    pos = torch.arange(past, past + n, device="cuda")
+    for got, x in ((q_out, q), (k_out, k), (K[:, :, past:].transpose(1, 2), k)):
+        assert torch.equal(got[..., rotary:].isnan(), x[..., rotary:].isnan())
+        assert torch.equal(got[..., rotary:].nan_to_num(7.0, math.inf, -math.inf), x[..., rotary:].nan_to_num(7.0, math.inf, -math.inf))
+        ref, size = rope64(x[0], None, 0, pos, freq, interleaved)
+        head = slice(0, rotary)
+        assert ((got[0, ..., head].double() - ref[..., head]).abs() <= rope_tolerance(ref, size, dtype)[..., head]).all()
+    assert torch.equal(V[:, :, past:].transpose(1, 2).contiguous().view(torch.int16), v.view(torch.int16))
+
+
 # --------------------------------------------------------------------------------------------- rows that few tokens dominate
 
 def check_by_tile(c, q, past, out, lse):
