@@ -430,7 +430,8 @@ int sik_attn_mass(const sik_layout *layout, const sik_chunk *chunk, const void *
  * With K_out and V_out (both or neither) the cache is cut down as well: rows keep[b,h,i] of K, V (contiguous, or paged by
  * `pages`; a token on an unmapped page gives a zero row) become rows i of K_out, V_out [B,Hkv,out_len,D], out_len >=
  * n_keep; rows beyond new_len are left as they were.  mass_out [B,Hkv,out_len] (may be NULL) receives their masses.  The
- * outputs must not overlap the inputs.  workspace: sik_chunk_workspace_bytes of the layout and any n. */
+ * outputs must not overlap the inputs or each other (new_len = seq_len is refused too: SIK_ERR_FLAGS).  workspace:
+ * sik_chunk_workspace_bytes of the layout and any n. */
 typedef struct {
     const float *mass;
     const int32_t *seq_len;

@@ -5,6 +5,11 @@ namespace sik {
 
 static bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
+static bool overlap(const void* p, size_t np, const void* q, size_t nq) {  // false where one is NULL
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return a != 0 && b != 0 && a < b + nq && b < a + np;
+}
+
 static int check_pages(const Dims& d, const sik_pages* p, CacheView* c) {
     *c = CacheView{nullptr, 0, 0, 0, d.Hkv, d.Lmax};
     if (!p) return SIK_OK;
@@ -138,6 +143,13 @@ int sik_evict(const sik_layout* layout, const sik_evict_args* a) {
     if ((a->K_out || a->mass_out) && a->out_len < a->n_keep) return SIK_ERR_CAPACITY;
     rc = check_chunk_ws(layout, 1, a->workspace, a->workspace_bytes);
     if (rc) return rc;
+    // workgroups read lengths and weights while others already write their part of the list
+    const size_t lens = static_cast<size_t>(d.B) * 4, list = static_cast<size_t>(d.units()) * a->n_keep * 4;
+    const size_t sums = static_cast<size_t>(d.units()) * d.Lmax * 4;
+    if (overlap(a->new_len, lens, a->seq_len, lens) || overlap(a->new_len, lens, a->mass, sums) ||
+        overlap(a->keep, list, a->seq_len, lens) || overlap(a->keep, list, a->mass, sums) ||
+        overlap(a->keep, list, a->new_len, lens))
+        return SIK_ERR_FLAGS;
     const EvictArgs e{a->mass, a->seq_len, a->n_keep, a->n_sink, a->n_recent, a->keep, a->new_len,
                       static_cast<const uint16_t*>(a->K), static_cast<const uint16_t*>(a->V),
                       static_cast<uint16_t*>(a->K_out), static_cast<uint16_t*>(a->V_out), a->mass_out, a->out_len};

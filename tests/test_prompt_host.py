@@ -176,3 +176,23 @@ def test_overlapping_tokens_are_refused():
     with pytest.raises(ValueError, match="^q: "):
         sik.sik_rope_append(lay, sik.make_chunk(4, torch.zeros(1, dtype=torch.int32)), q, k, torch.zeros(1, 4, 8, 128, dtype=torch.bfloat16),
                             k_out=torch.zeros_like(k))
+
+
+def test_evict_refuses_lists_and_lengths_over_its_inputs():
+    # a workgroup may still have to read what another one has overwritten
+    lay = L(max_len=64)  # 2 x 2 rows of 64 weights, 1024 bytes; two lengths, 8; lists of 16 tokens, 256
+    base, far = 256 * 1000, 256 * 2000
+
+    def call(**kw):
+        a = dict(mass=base, seq_len=far, new_len=far + 1024, keep=far + 4096, n_keep=16, workspace=far * 2, workspace_bytes=1 << 40)
+        a.update(kw)
+        return sik.lib().sik_evict(P(lay), P(sik.EvictArgs(**a)))
+
+    for at in (far, far + 4, far - 4):
+        assert call(new_len=at) == -8
+    for at in (base, base + 1020, base - 4):
+        assert call(new_len=at) == -8
+    for at in (far, far + 4, far - 252, base, base + 1020, base - 252, far + 1024, far + 1028, far + 1024 - 252):
+        assert call(keep=at) == -8
+    if not torch.cuda.is_available():  # beside each other: as far as the launch, for which there is no device
+        assert call(new_len=far + 8, keep=far + 16) == -7 and call(new_len=base + 1024, keep=base - 256) == -7
