@@ -396,6 +396,57 @@ def test_evict(B, Hkv, lengths, n_keep, n_sink, n_recent, page, dtype, kind):
     assert torch.equal(only, keep) and torch.equal(alone, mo)
 
 
+def keep_sorted(mass, n_keep, n_sink, n_recent):
+    """mass [rows, L] -> indices that stay [rows, min(L, n_keep)], ascending, from a stable sort on the device."""
+    rows, L = mass.shape
+    if L <= n_keep:
+        return torch.arange(L, device="cuda").expand(rows, -1)
+    best = torch.sort(mass[:, n_sink:L - n_recent], dim=-1, descending=True, stable=True)[1][:, :n_keep - n_sink - n_recent]
+    ends = [torch.arange(*x, device="cuda").expand(rows, -1) for x in ((0, n_sink), (L - n_recent, L))]
+    return torch.cat([ends[0], best.sort(dim=-1)[0] + n_sink, ends[1]], -1)
+
+
+MANY = [
+    # B, Hkv, max_len, n_keep, n_sink, n_recent
+    (16, 4, 16380, 500, 4, 64),     # four steps of 4096 tokens in a workgroup's registers
+    (8, 8, 20000, 19999, 0, 1),     # five
+    (16, 8, 24000, 1000, 100, 0),   # six
+    (24, 8, 28673, 64, 0, 0),       # eight, of which the last one is almost empty
+    (48, 4, 32768, 4096, 1, 1),     # eight
+    (5, 8, 32769, 300, 4, 30),      # three launches: rows that share counts, lists and heads
+    (65, 4, 32800, 2000, 0, 64),    # a workgroup per row there too, most of its weights not in registers
+    (2, 2, 90001, 5000, 10, 10),
+]
+
+
+@pytest.mark.parametrize("kind", ["plain", "equal", "steps"])
+@pytest.mark.parametrize("B,Hkv,cap,n_keep,n_sink,n_recent", MANY)
+def test_evict_many_rows(B, Hkv, cap, n_keep, n_sink, n_recent, kind):
+    # every form of the selection, in batches; sequences from none to max_len tokens, some no longer than what is kept
+    gen = gen_of(B, cap, n_keep)
+    lengths = [[cap, n_keep, 0, n_keep + 1, cap - 1][b] if b < 5 else int(cap ** (b / B)) for b in range(B)]
+    mass = torch.exp(2 * torch.randn(B, Hkv, cap, generator=gen, device="cuda"))
+    if kind == "equal":
+        mass[:] = 3.0
+    elif kind == "steps":
+        mass = mass.round()
+    for b, L in enumerate(lengths):
+        mass[b, :, L:] = math.nan
+    lay = sik.make_layout(B, Hkv, Hkv, D, cap, BF)
+    size = sik.sik_chunk_workspace_bytes(lay, 1)
+    ws = torch.full((size + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    keep = torch.full((B, Hkv, n_keep), -5, dtype=torch.int32, device="cuda")
+    new_len, mo = ints([-1] * B), torch.full((B, Hkv, n_keep + 3), 7.0, device="cuda")
+    sik.sik_evict(lay, mass, ints(lengths), n_keep, keep, ws[:size], n_sink=n_sink, n_recent=n_recent, new_len=new_len, mass_out=mo)
+    assert new_len.tolist() == [min(L, n_keep) for L in lengths]
+    assert (ws[size:] == 0xA5).all()
+    for b, L in enumerate(lengths):
+        m = min(L, n_keep)
+        want = keep_sorted(mass[b, :, :L], n_keep, n_sink, n_recent)
+        assert torch.equal(keep[b, :, :m].long(), want) and (keep[b, :, m:] == -1).all(), (b, L)
+        assert torch.equal(mo[b, :, :m], torch.gather(mass[b], 1, want)) and (mo[b, :, m:] == 7).all()
+
+
 def test_tensors_on_another_device_are_refused():
     lay = sik.make_layout(1, 1, 2, D, 64, BF)
     K = torch.zeros(1, 1, 64, D, dtype=BF, device="cuda")
