@@ -32,9 +32,11 @@ constexpr int kMaxParts = 128;   // workgroups that share one row tile's cache
 //   2^kUnder below the largest logit, and moves down as well, to the largest logit of a tile that is more than 2^kDrop (binary32
 //   results: kDropPrec) below: a tile's largest weight is then at least 2^(kUnder - kDrop), and what the tile's 64 tokens lose
 //   at the lower end is at most 2^-14 (2^-18) of that one.  At most 2^kDepth down from the highest reference: a row of 2^22 tokens
-//   of weights below 2^(15 + kDepth) and values below 2^16 stays within binary32.  These references are whole numbers, so that
-//   moving one, any number of times, rounds nothing.  The downward moves cost 1 % of a prompt's time (2048 tokens behind 6144,
-//   8/32 heads: 258 us against 255) and 4 % with binary32 results (353 against 340; 366 with kDropPrec 4, 356 with 6).
+//   of weights below 2^(15 + kDepth) and values below 2^16 stays within binary32.  The downward moves cost 1 % of a prompt's
+//   time (2048 tokens behind 6144, 8/32 heads: 260 us against 257) and 4 % with binary32 results (352 against 340; 366 with
+//   kDropPrec 4, 356 with 6).
+// Either way the weight of the logit that m was taken from is a power of two, which 16 bits hold exactly: where one token has
+// most of a row's weight, that rounds nothing.
 constexpr float kSlack = 8.0f, kUnder = 7.0f, kDrop = 12.0f, kDropPrec = 8.0f, kDepth = 60.0f;
 
 struct ChunkAttn {
@@ -110,16 +112,13 @@ __device__ __forceinline__ bool has_to_move(const RowState& st, float top) {
 
 template <int DT, bool PREC>
 __device__ __forceinline__ void rescale(RowState& st, float top) {
-    float m, f;
-    if constexpr (DT != kF16) {
-        m = fmaxf(st.m, top);
-        f = fast_exp2(st.m - m);
-    } else {
-        m = ceilf(top) - kUnder;
+    float m = fmaxf(st.m, top);
+    if constexpr (DT == kF16) {
+        m = top - kUnder;
         m = m > st.m ? m : has_to_move<DT, PREC>(st, top) ? fmaxf(m, st.hi - kDepth) : st.m;
-        f = __builtin_amdgcn_ldexpf(1.0f, static_cast<int>(fmaxf(st.m - m, -200.0f)));
         st.hi = fmaxf(st.hi, m);
     }
+    const float f = fast_exp2(st.m - m);
     st.m = m;
     st.l *= f;
 #pragma unroll
