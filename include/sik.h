@@ -405,10 +405,10 @@ size_t sik_chunk_workspace_bytes(const sik_layout *layout, int32_t n);
  *   out[b,t,hq] = sum_j p_j V_j, p = softmax over the tokens j <= seq_len[b] + t of softmax_scale * q[b,t,hq] . K_j
  * q [B,n,Hq,D] kv_dtype, out [B,n,Hq,D] out_dtype, lse [B,n,Hq] float or NULL: the natural logarithm of the softmax's
  * sum.  softmax_scale <= 0 means 1 / sqrt(D).  A row without any token (all its pages are unmapped) gives a zero row and
- * lse = -infinity.  Products on the matrix units with binary32 sums; a weight is rounded once to kv_dtype for the second one
- * (out_dtype binary32: what that drops is added as a second number of kv_dtype), which for fp16 is at most 2^-20 (2^-24) of the
- * largest weight of the 64 tokens around it where that exceeds 2^-11 (2^-22) of itself.  K, V and q must be finite in every
- * valid row. */
+ * lse = -infinity.  Products on the matrix units with binary32 sums.  For the second one a weight is rounded once to kv_dtype;
+ * where out_dtype is binary32, or n * R <= 32, what that drops is added as a second number of kv_dtype.  fp16 weights far below
+ * those around them are held to 2^-20 (second number: 2^-24) of the largest among 64 tokens.  K, V and q must be finite in
+ * every valid row. */
 int sik_chunk_attn(const sik_layout *layout, const sik_chunk *chunk, const void *q, const void *K, const void *V,
                    float softmax_scale, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
 

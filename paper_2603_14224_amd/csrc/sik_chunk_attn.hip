@@ -129,10 +129,12 @@ __device__ __forceinline__ void rescale(RowState& st, float top) {
 
 // A tile's weights as operands, a group of 16 tokens in each.  The matrix units take both operands in the values' type, so a
 // weight is rounded to 16 bits, by at most 2^-8 (bf16) or 2^-11 (fp16; below 2^-14 by 2^-25, see the references above) of itself,
-// half of its step, up or down, so that a row's result is off by about as much as by its own rounding to that type (both together,
-// root mean square over prompts of random rows: bf16 2.1e-3 of the result, 1.6e-3 of it the result's own; fp16 2.9e-4 and 2.1e-4;
-// a second operand for the rest takes 1.35 times as long).  The sum that divides it is taken before the rounding.  PREC (binary32
-// results): what the rounding dropped is a second operand.
+// half of its step, up or down.  The sum that divides it is taken before the rounding.  PREC: what the rounding dropped is a second
+// operand.  The `rows` form has it for binary32 results only: with 16-bit ones a row is off by about as much through the weights
+// as through its own rounding (root mean square over prompts of random rows: bf16 2.2e-3 of the result against 1.65e-3 with
+// the second operand, fp16 2.8e-4 against 2.1e-4; a single row can be off by twice as much), and the second operand takes 1.35
+// times as long.  The `tokens` form always has it, beside loads that take longer: 8 tokens behind 32760 of 8/32 heads 38.3 us
+// against 37.8, 32 x 4 behind 4000 of 8/64 134.2 against 132.9.
 template <int NK, bool PREC>
 struct Weights {
     u32x4 w[2 * NK], rest[PREC ? 2 * NK : 1];
@@ -419,8 +421,8 @@ __global__ __launch_bounds__(kBlock, 2) void chunk_tokens_kernel(const ChunkAttn
         else
             dma_wait<0>();
         const float top = tile_top<1>(s, a.scale_log2e);
-        if (__any(has_to_move<DT, ODT == kF32>(st, top))) rescale<DT, ODT == kF32>(st, top);
-        Weights<1, ODT == kF32> w;
+        if (__any(has_to_move<DT, true>(st, top))) rescale<DT, true>(st, top);
+        Weights<1, true> w;
         tile_weights<DT, 1>(st, s, a.scale_log2e, w);
         tile_values<DT, 1>(st, w, values, lane);
         lds_reads_done();

@@ -780,3 +780,20 @@ def test_chunk_attn_far_tokens_of_an_unsplit_cache(n, past, dtype, out_dtype):
     check_by_tile(c, q, past, out[7:8], lse[7:8])
     for x in (out, lse):
         assert torch.equal(x, x[7:8].expand_as(x))
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("n,Hkv,R,past,page", [(1, 2, 3, 300, 0), (1, 2, 1, 40, 16), (1, 8, 4, 9663, 0), (4, 2, 4, 3449, 64), (32, 1, 1, 70, 0)])
+def test_chunk_attn_few_rows_are_rounded_once(n, Hkv, R, past, page, dtype):
+    # up to 32 rows per KV head: 16-bit results are those in binary32, rounded.  A value's distance to the nearest number of
+    # the type changes by no more than the value does, so the result is off by that distance of the exact value and twice the
+    # error of the binary32 one.
+    gen = gen_of(n, past, 5)
+    c = Cache(1, Hkv, past + n, dtype, page, [past + n], gen)
+    q = randn((1, n, Hkv * R, D), gen, dtype, scale=0.5)
+    out, _ = run_chunk(sik.make_layout(1, Hkv, Hkv * R, D, past + n, dtype), c, q, [past], None, n)
+    k, there = c.rows(c.K, 0, past + n)
+    v, _ = c.rows(c.V, 0, past + n)
+    r = attn64(q[0], k, v, there, past, SCALE)
+    nearest = (r["out"].to(dtype).double() - r["out"]).abs()
+    assert ((out[0].double() - r["out"]).abs() <= nearest + 2 * out_tolerance_by_tile(r, v, dtype, torch.float32)).all()
