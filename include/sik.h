@@ -54,7 +54,7 @@ typedef enum {
     SIK_ERR_CAPACITY = -5,  /* token range outside [0, max_len]                              */
     SIK_ERR_WORKSPACE = -6, /* workspace NULL, misaligned or smaller than sik_workspace_bytes */
     SIK_ERR_LAUNCH = -7,    /* the HIP runtime reported an error while enqueueing           */
-    SIK_ERR_FLAGS = -8,     /* unknown quantiser mode, or an option value out of range      */
+    SIK_ERR_FLAGS = -8,     /* unknown quantiser mode, an option value out of range, or an output over an input */
     SIK_ERR_STATIC_LIMIT = -9, /* sik_decode_step_static: the layout needs more scratch memory than the
                                  library's built-in buffer holds (SIK_STATIC_SCRATCH_BYTES)       */
     SIK_ERR_ALIGN = -10     /* a pointer or stride of the prompt-side calls is not 16-byte aligned        */
@@ -375,7 +375,8 @@ typedef struct {
  * rotated.  position = seq_len[b] + t, or positions[b][t] ([B,n] int32) where given (a cache that tokens were evicted
  * from: rows and positions differ).  The angle is the exact product, reduced to a turn in 64 bits; everything else is
  * binary32, rounded once to kv_dtype.
- * Tokens of q, k and v lie q_stride, k_stride, v_stride elements apart (0: packed, heads * D), sequences n times that, so
+ * Tokens of q, k and v lie q_stride, k_stride, v_stride elements apart (0: packed, heads * D; not less than that: one row
+ * cannot stand for several tokens), sequences n times that, so
  * that they may be parts of one projection's output; a head's D values and the heads of a token are contiguous.
  * q_out [B,n,Hq,D].  Keys go to k_out [B,n,Hkv,D] (a decode step's k_new, v then is used as it is: v = K = V = NULL) or,
  * with the values of v, into the cache K, V (k_out = NULL).  Outputs must not overlap inputs (q_out = q and k_out = k are

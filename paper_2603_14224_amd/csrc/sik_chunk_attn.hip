@@ -12,9 +12,9 @@
 // tokens, and the four states of a workgroup are joined at the end.  Either form splits the cache over several workgroups
 // where there are too few to fill the chip; a second launch joins their states.
 //
-// Bounds: few rows, memory (one token of 32 heads on 32767 tokens, 134 MB: 22 us and 5 for the join); many, matrix and vector
-// instructions in turn at a clock that falls under the load (8192-token prompt of 32 heads 528 us, 1.04 PFLOP/s; 2048 tokens
-// behind 30720 1001 us, 1.06; a plain product of the library 1.2).
+// Bounds: few rows, memory (one token of 32 heads on 32767 tokens, 134 MB: 23 us and 5 for the join); many, matrix and vector
+// instructions in turn at a clock that falls under the load (8192-token prompt of 32 heads 533 to 550 us, 1.00 to 1.03 PFLOP/s;
+// 2048 tokens behind 30720 1010 us, 1.05; a plain product of the library 1.2).
 #include "sik_attn_core.h"
 #include "sik_mma.h"
 
@@ -503,7 +503,7 @@ __global__ __launch_bounds__(kBlock) void join_tokens_kernel(const ChunkAttn a) 
     for (int x = 32; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
 #pragma unroll
     for (int i = 0; i < kMaxParts / 64; ++i) {
-        const float f = ml[i].y > 0.0f ? fast_exp2(ml[i].x - M) : 0.0f;  // a part without tokens has not written its rows
+        const float f = ml[i].y > 0.0f ? fast_exp2(ml[i].x - M) : 0.0f;  // a part without tokens gives nothing
         l += ml[i].y * f;
         if (tid < 64) s_f[lane + 64 * i] = f;
     }
@@ -617,7 +617,7 @@ struct ChunkPlan {
     int tiles, parts, tile_rows;
 };
 // At least 256 tokens to a part; of short caches in the `tokens` form 128, a step of its four wavefronts, up to 32 parts (one
-// token on 500 to 4000 tokens of 8 KV heads 9.3 to 9.9 us against 10.5 to 11.1; on 8000 63 parts take 12.9, 32 take 11.7).
+// token on 500 to 2000 tokens of 8 KV heads 9.2 to 10.2 us against 10.3 to 11.3; on 8000 63 parts take 15.7, 32 take 14.8).
 static int most_parts(const Dims& d, bool tokens) {
     int most = (d.Lmax + 255) / 256;
     if (tokens && most < 32) most = (d.Lmax + 127) / 128 < 32 ? (d.Lmax + 127) / 128 : 32;
@@ -633,8 +633,9 @@ static ChunkPlan chunk_plan(const Dims& d, int n) {
     p.parts = 1;
     const int most = most_parts(d, p.tokens);
     if (p.tokens) {
-        // memory-bound: one round of workgroups (one token on 32767 tokens of 8 KV heads: 28 us in 64 parts, 31 in 96; on 8000
-        // 11.7 us in 32 parts, 44 in two)
+        // memory-bound: one round of workgroups (one token on 32767 tokens of 8 KV heads: 33 us in 64 parts, 38 in 96; on 1000 of
+        // 32 x 8 heads 33.8 in two, 36.6 in three).  From 257 units on that is one part, which leaves up to half of the round
+        // empty: a token on 1000 of 33 x 8 heads 38.2 in one, 37.3 in two, on 8000 278 and 249.
         const int64_t by_slots = kSlots / groups;
         p.parts = static_cast<int>(by_slots < 1 ? 1 : by_slots < most ? by_slots : most);
         return p;
@@ -642,8 +643,8 @@ static ChunkPlan chunk_plan(const Dims& d, int n) {
     // Cost of a split in tiles of 64 tokens, a part's state and its join counted as six (a lone part's start as two): rounds
     // of workgroups, as if all sequences were as long as the cache; in a batch, where they seldom are, plus the same with
     // lengths spread (two thirds on average, half of the last round idle).  333 tokens behind 9000 of 6 x 8 KV heads with
-    // 5:1 heads: two parts 464 us against 516 of one, with unequal lengths 247 against 274; 100 behind 16000 of 8 x 8 with
-    // 8:1, unequal: 270 against 436; 64 behind 2000 of 16 x 8 with 4:1: two parts 56, four 66.
+    // 5:1 heads: two parts 457 us against 468 of one, with unequal lengths over pages 250 against 305; 100 behind 16000 of 8 x 8
+    // with 8:1, unequal: 270 against 357; 64 behind 2000 of 16 x 8 with 4:1: two parts 63, one 61, four 73.
     const float T = static_cast<float>((d.Lmax + 63) / 64);
     float best = 0.0f;
     for (int k = 1; k <= most && (k == 1 || groups * k <= kMaxGroups); ++k) {

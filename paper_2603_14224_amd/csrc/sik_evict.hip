@@ -7,8 +7,8 @@
 // up, finds the cut's bin and writes its tokens of that bin, a few per cent, behind those of the chunks before), `place` (the
 // other two digits from those tokens alone, then the chunk's part of the list).
 //
-// Bounds: the list, chains of memory, counting and barriers (one row of 65536 weights in 19.5 us, 32 of them in 31; 256 rows of
-// 16370 in 23); the rows, memory (2048 rows of K and V for each of 256, 537 MB: 87 us, 6.2 TB/s).
+// Bounds: the list, chains of memory, counting and barriers (one row of 65536 weights in 18.5 us, 32 of them in 28; 256 rows of
+// 16370 in 22); the rows, memory (2048 rows of K and V for each of 256, 537 MB: 87 us, 6.2 TB/s).
 #include "sik_chunk.h"
 
 namespace sik {
@@ -18,7 +18,7 @@ constexpr int kDigitBins = 2048;   // of the first two digits; the last one has 
 constexpr int kChunkTokens = 4096; // the fewest tokens of a chunk
 constexpr int kEvictChunks = 64;   // the most chunks of a row, whose counts every workgroup adds up
 // Compute units.  A second round of workgroups costs more than longer chunks: 32 rows of 65544 weights in nine chunks of 8192
-// took 39 us, in eight of 8256 31.
+// take 37 us, in eight of 8256 28.
 constexpr int kEvictUnits = 256;
 constexpr int kEvictStep = 4096;   // tokens of a workgroup at four weights per thread
 
@@ -456,9 +456,9 @@ __global__ __launch_bounds__(kBlock) void evict_rows_kernel(EvictArgs a, CacheVi
 }
 
 // One workgroup per row up to 12288 tokens, up to 32768 from as many rows on as the chip has no room to split (us against the
-// three launches): 12000 tokens, 1 row 17.1 / 17.5, 256 rows 18.5 / 28.6; 16370, 1 row 21.0 / 17.6, 64 rows 21.4 / 21.2, 256
-// rows 22.9 / 35.2; 20000, 128 rows 25.5 / 28.9; 24000, 128 rows 30 / 29.9, 256 rows 31 / 45; 32000, 128 rows 40 / 35, 256
-// rows 42 / 58.
+// three launches): 12000 tokens, 1 row 16.0 / 16.4, 256 rows 19.4 / 29.4; 16370, 1 row 19.7 / 16.6, 64 rows 21.2 / 19.3, 128
+// rows 22.1 / 23.2, 256 rows 24.1 / 35.6; 20000, 64 rows 25.4 / 23.1, 128 rows 26.8 / 29.2; 24000, 64 rows 29.7 / 23.5, 128 rows
+// 31.5 / 29.6, 192 rows 32.4 / 44.6; 32000, 128 rows 41.8 / 35.4, 192 rows 43.0 / 57.4.
 static bool evict_direct(const Dims& d) {
     const int steps = (d.Lmax + kEvictStep - 1) / kEvictStep;
     return steps <= 3 || (steps <= 8 && d.units() >= (steps <= 5 ? 64 : steps <= 6 ? 128 : 192));

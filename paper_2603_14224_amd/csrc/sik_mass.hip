@@ -5,15 +5,15 @@
 // (column l % 32) and half of the tile's queries in its registers, so the weights are summed in the lane: no exchange, no
 // atomics, one order of additions.  Rows as in chunk attention: token t of the chunk and head r of the group are row t R + r.
 //
-// Bounds: one query per sequence, the keys (8 x 16384 tokens of 8 KV heads, 276 MB: 46 us, 5.9 TB/s); many, products and
-// exponentials (256 queries of 32 heads on 32768 tokens: 88 us, 775 TFLOP/s; matrix units busy a third of the time, vector
-// units more than half).  Eight wavefronts to a workgroup, not four: a tile's load is one instruction to each of them (these two
-// 50 and 91 us with four, 4 x 8 heads with 5:1, 100 queries on 8000 tokens 51 against 57).
+// Bounds: one query per sequence, the keys (8 x 16384 tokens of 8 KV heads, 276 MB: 50 us, 5.5 TB/s; 66 over changing tensors);
+// many, products and exponentials (256 queries of 32 heads on 32768 tokens: 90 us, 760 TFLOP/s; matrix units busy a third of the
+// time, vector units half).  Eight wavefronts to a workgroup, not four: a tile's load is one instruction to each of them (these
+// two took 8 and 3 % longer with four; 100 queries on 8000 tokens of 4 x 8 heads with 5:1 12 %).
 #include "sik_mma.h"
 
 namespace sik {
 
-constexpr int kMassFull = 160;   // workgroups of 128 tokens below which four wavefronts share 32
+constexpr int kMassFull = 160;   // halves of workgroups, 128 tokens each, below which four wavefronts share 32 tokens
 constexpr int kMassBlock = 512, kMassKeys = kMassBlock / kWave * 32;  // threads and tokens of a workgroup
 constexpr int kMassRows = 32;    // query rows of a tile
 constexpr int kMassBuffers = 4;  // tiles in LDS
@@ -242,9 +242,10 @@ __global__ __launch_bounds__(kBlock, 2) void mass_split_kernel(const MassArgs a)
 
 hipError_t launch_mass(const Dims& d, const CacheView& c, const ChunkView& ch, const void* q, const void* K, float scale,
                        const float* lse, int n_obs, const float* before, float* mass, hipStream_t s) {
-    // shared tokens where the workgroups of 128 would leave compute units idle and there are queries for all four wavefronts:
-    // 8 KV heads with 4:1 heads, 256 queries on 1000 tokens (64 workgroups) 15.4 us against 24.9, 2048 on the same 2048 (136)
-    // 133 against 193; but 256 on 3500 (224) 34 against 30
+    // shared tokens where workgroups of 256 tokens would leave most compute units idle and there are queries for all four
+    // wavefronts.  8 KV heads with 4:1 heads, shared against not: 256 queries on 1264 tokens (80 halves of workgroups) 18 us and
+    // 30, on 2264 (144) 28 and 28, on 2764 (176) 31 and 29, on 4264 (272) 42 and 31; 2048 on 2556 (160) 140 and 193, on 3056 (192)
+    // 195 and 192.  One KV head, 64 queries on 16072 tokens (126) 7.9 and 11.1, on 20072 (157) 11.7 and 10.7.
     const int64_t wide = (d.Lmax + 127) / 128 * static_cast<int64_t>(d.units());
     const bool split = wide < kMassFull && static_cast<int64_t>(n_obs) * d.R > 2 * kMassRows;
     const int blocks = split ? (d.Lmax + 31) / 32 : (d.Lmax + kMassKeys - 1) / kMassKeys;

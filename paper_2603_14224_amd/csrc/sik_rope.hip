@@ -5,10 +5,10 @@
 // are paired with: the same 16 bytes of another lane, loaded a second time (from the first-level cache) rather than
 // exchanged.  The angles of a token are the same for all its heads: a wavefront computes them once, in front of its steps.
 //
-// Bound by memory: 8192 tokens of 40 rows rotated and 8 copied, 201 MB, in 41 us where the outputs stay in the Infinity Cache
+// Bound by memory: 8192 tokens of 40 rows rotated and 8 copied, 201 MB, in 40 us where the outputs stay in the Infinity Cache
 // and in 53 to 57 where they do not (3.5 TB/s; a copy reaches 4.7).  Requests one step ahead (76 us), two steps at a time
 // (62), the partners exchanged between lanes (70) and streaming stores on top of these (66 to 72) were all slower there; one
-// token takes 3.5 us.
+// token takes 3.6 us.
 #include "sik_chunk.h"
 
 namespace sik {
