@@ -409,7 +409,7 @@ size_t sik_chunk_workspace_bytes(const sik_layout *layout, int32_t n);
  * lse = -infinity.  Products on the matrix units with binary32 sums.  For the second one a weight is rounded once to kv_dtype;
  * where out_dtype is binary32, or n * R <= 32, what that drops is added as a second number of kv_dtype.  fp16 weights far below
  * those around them are held to 2^-20 (second number: 2^-24) of the largest among 64 tokens.  K, V and q must be finite in
- * every valid row. */
+ * every valid row, logits (softmax_scale * q . K_j) below 2^22 in size. */
 int sik_chunk_attn(const sik_layout *layout, const sik_chunk *chunk, const void *q, const void *K, const void *V,
                    float softmax_scale, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
 
